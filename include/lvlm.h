@@ -55,7 +55,8 @@ typedef enum {
     LVLM_OP_DECODE_ATTN = 3,
     LVLM_OP_MERGE_SIMILAR = 4,
     LVLM_OP_SCORE_PROBS = 5,
-    LVLM_OP_PREFILL_ATTN = 6
+    LVLM_OP_PREFILL_ATTN = 6,
+    LVLM_OP_TREE_ATTN = 7
 } lvlm_op;
 
 /* Rank -> weight tables for the merged token (Sec. 3.2.1, par. 4). */
@@ -441,6 +442,120 @@ LVLM_API lvlm_status lvlm_decode_attn_static(lvlm_ctx *ctx, void *stream, const 
                                     const void *q, const void *k_new, const void *v_new,
                                     void *k_cache, void *v_cache, float *score, uint8_t *kind,
                                     int32_t *orig_pos, int32_t *len, void *out);
+
+/* ---- drafted tokens: several entries at once, caches in pages ------------- */
+
+/* A cache as the calls below take it (HOST struct of device pointers).  Without pages it is the head-major layout above.
+ * With pages the heads draw their slots from one pool, so that after compression, which leaves every head a length of
+ * its own, memory follows what the heads hold:
+ *   k, v      [n_pages, page_size, hd]        score, kind, orig_pos  [n_pages, page_size]
+ *   pages     [B, Hkv, Lmax / page_size] i32  slot s of head (b, g) is place s % page_size of page
+ *                                             pages[b][g][s / page_size]
+ * Only table places below a head's length (the new one, when appending) are read.  A page number outside [0, n_pages)
+ * holds nothing: entries written there are dropped, entries read there are not seen, and no memory is touched. */
+typedef struct {
+    void *k, *v;
+    float *score;         /* score, kind, orig_pos may be NULL: then they are not kept      */
+    uint8_t *kind;
+    int32_t *orig_pos;
+    const int32_t *pages; /* NULL: head-major                                               */
+    int32_t Lmax;         /* slots per head; with pages a multiple of page_size             */
+    int32_t page_size;    /* with pages: a power of two, 16 .. 65536; else 0                */
+    int32_t n_pages;      /* with pages: >= 1; else 0                                       */
+    int32_t reserved;     /* 0                                                              */
+} lvlm_cache;
+
+typedef struct {
+    int32_t dtype;        /* LVLM_BF16 or LVLM_F32: new rows, q, caches                     */
+    int32_t B, T;         /* sequences, new rows per sequence at most (0: none)             */
+    int32_t Hq, Hkv;      /* query heads (read only with q), KV heads                       */
+    int32_t hd;           /* 64 or 128                                                      */
+    int32_t rot_dim;      /* channels that turn: a multiple of 16 up to hd; 0 = none        */
+    int32_t adjacent;     /* 0: channel i turns with i + rot_dim/2; 1: 2i with 2i+1         */
+    int32_t n_axes;       /* position axes, 1 .. 3 (read only with rot_dim > 0)             */
+    int32_t sections[3];  /* pairs of each axis, in order; they add up to rot_dim / 2       */
+    int32_t new_kind;     /* kind of the entries where src->kind is NULL                    */
+    int32_t reserved;     /* 0                                                              */
+    int64_t k_stride_b, k_stride_t, k_stride_h;    /* k[b][t][g][0..hd), elements           */
+    int64_t v_stride_b, v_stride_t, v_stride_h;    /* v[b][t][g][0..hd)                     */
+    int64_t q_stride_b, q_stride_t, q_stride_h;    /* q[b][t][h][0..hd)                     */
+    int64_t qo_stride_b, qo_stride_t, qo_stride_h; /* q_out[b][t][h][0..hd)                 */
+    int64_t n_stride_b, n_stride_h;                /* n_new[b][g]; n_stride_h 0: one count per sequence */
+    int64_t m_stride_b, m_stride_h;                /* score / kind / orig_pos[b][g][t]; m_stride_h 0: shared by the heads */
+} lvlm_append_desc;
+
+typedef struct {          /* HOST struct of device pointers                                  */
+    const void *k, *v;
+    const void *q;        /* NULL: keys only                                                */
+    void *q_out;          /* may be q itself with the same strides                          */
+    const int32_t *pos;   /* [n_axes, B, T] dense; needed to turn                           */
+    const float *inv_freq;/* [rot_dim / 2] fp32; needed to turn                             */
+    const int32_t *n_new; /* rows in use (strides above); NULL: T                           */
+    const float *score;   /* the entries' importance; NULL: 0                               */
+    const uint8_t *kind;  /* NULL: new_kind                                                 */
+    const int32_t *orig_pos; /* NULL: axis 0 of pos, without pos the row number t           */
+} lvlm_append_src;
+
+/* Appends n = n_new[b][g] (clamped to [0, T]) entries to every head's list: row t goes to slot len[b][g] + t, t < n, and
+ * len_out[b][g] = len[b][g] + n.  On the way keys and queries are turned by their position: pair c of the rot_dim / 2
+ * pairs, of axis a by the sections, turns by the angle pos[a][b][t] * inv_freq[c],
+ *   x_i' = x_i cos - x_j sin,  x_j' = x_j cos + x_i sin,
+ * angles reduced in 64 bits (exact at any 32-bit position), products in fp32, one rounding to the dtype; channels from
+ * rot_dim on, and values, are copied.  q_out[b][t] for t < n; rows from n on are neither read nor written.
+ * A head whose entries do not all fit (len + n > Lmax, or a negative len) takes none of them and keeps its length: a caller
+ * that cannot rule this out compares the lengths.  Without turning and with counts per head the call packs compressed lists,
+ * with their score, kind and orig_pos, into pages.  len_out may be len itself.  q needs counts per sequence (n_stride_h 0) and
+ * rot_dim > 0.  New rows must not overlap the cache.  No workspace. */
+LVLM_API lvlm_status lvlm_kv_append(lvlm_ctx *ctx, void *stream, const lvlm_append_desc *d, const lvlm_append_src *src,
+                                    const lvlm_cache *cache, const int32_t *len, int32_t *len_out);
+
+typedef struct {
+    int32_t dtype;     /* LVLM_BF16 or LVLM_F32: q, caches, out                             */
+    int32_t B, T;      /* sequences, drafted rows per sequence at most: 1 .. 1024           */
+    int32_t Hq, Hkv;   /* query heads, KV heads (Hq % Hkv == 0, Hq / Hkv * T < 65536)       */
+    int32_t hd;        /* 64 or 128                                                         */
+    int32_t Lmax;      /* that of the cache                                                 */
+    int32_t len_bound; /* host-known upper bound of every len (0 = Lmax); sizes the launch  */
+    float scale;       /* logit scale > 0, usually 1/sqrt(hd)                               */
+    int32_t reserved;  /* 0                                                                 */
+    int64_t q_stride_b, q_stride_t, q_stride_h; /* q[b][t][h][0..hd), elements              */
+    int64_t o_stride_b, o_stride_t, o_stride_h; /* out[b][t][h][0..hd)                      */
+} lvlm_tree_desc;
+
+/* Attention of a tree of drafted tokens over the cache that already holds them.  With n = n_rows[b] (clamped to [0, T];
+ * NULL: T) the last n of a head's len[b][g] entries are the drafted rows 0 .. n-1; row t sees every entry before them and
+ * the drafted rows i with bit i % 32 of mask[b][t][i / 32] set (mask [B, T, ceil(T / 32)] u32; NULL: the rows i <= t, a
+ * chain).  For t < n and query head h of KV head g, over the entries j that row t sees:
+ *   out[b][t][h] = sum_j softmax_j(scale q[b][t][h] . k_j) v_j,   row_lse[b][h][t] = ln sum_j exp(scale q . k_j)
+ * softmax and sums in fp32 (bf16: probabilities are rounded to bf16 for the product with the values).  A row that sees nothing
+ * writes zeros and -inf; rows from n on are left as they were.  What a row does not see adds nothing to it, whatever it holds
+ * (NaN and infinities included).  T = 1 is plain decoding from such a cache.  Entries at or beyond len_bound are not read.
+ * q is turned already (lvlm_kv_append).  row_lse [B, Hq, T] fp32 may be NULL.  out must not overlap q or the cache.
+ * The importance of the entries is left as it is.  Workspace: LVLM_OP_TREE_ATTN. */
+LVLM_API lvlm_status lvlm_tree_attn(lvlm_ctx *ctx, void *stream, const lvlm_tree_desc *d, const void *q,
+                                    const lvlm_cache *cache, const int32_t *len, const int32_t *n_rows,
+                                    const uint32_t *mask, void *out, float *row_lse);
+
+/* Visibility words of a tree: parent[t] is the row before row t on its path, in [-1, t) (-1: a root); row t sees itself
+ * and its ancestors.  mask_out: T * ceil(T / 32) words.  HOST memory, 1 <= T <= 1024. */
+LVLM_API lvlm_status lvlm_tree_mask(int T, const int32_t *parent, uint32_t *mask_out);
+
+typedef struct {
+    int32_t dtype;     /* LVLM_BF16 or LVLM_F32                                             */
+    int32_t B, Hkv;
+    int32_t hd;        /* 64 or 128                                                         */
+    int32_t P;         /* places of path per sequence: 1 .. 65536                           */
+    int32_t reserved;  /* 0                                                                 */
+} lvlm_commit_desc;
+
+/* Keeps the accepted path of drafted rows: len[b][g] are the lengths before the drafts, path[b][0 .. n_path[b]) strictly
+ * ascending drafted rows (n_path is clamped to [0, P]).  In every head the entry (k, v, score, kind, orig_pos) of slot
+ * len + path[b][i] moves to slot len + i, and len_out = len + n_path.  A path that stops ascending, turns negative or leaves
+ * the Lmax slots ends before that place; a head with a negative len, or none of whose slots are left, keeps its length.
+ * An entry that would move from or to a page outside the pool is left.
+ * path [B, P] i32, n_path [B] i32 (device).  len_out may be len itself.  No workspace. */
+LVLM_API lvlm_status lvlm_tree_commit(lvlm_ctx *ctx, void *stream, const lvlm_commit_desc *d, const lvlm_cache *cache,
+                                      const int32_t *len, const int32_t *path, const int32_t *n_path, int32_t *len_out);
 
 /* Diagnostic, not part of the path: one read-only pass over `bytes` (a multiple of 16) of device memory at src by
  * n_workgroups workgroups of 256 threads (contiguous shares, 16-byte loads, eight in flight per thread), timed like

@@ -640,3 +640,162 @@ def decode_attn(q, k_new, v_new, k_cache, v_cache, score, kind, orig_pos, length
                 new = decay * np.asarray(score[b, g, :L], dtype=np.float64) + p_sum / G
                 score[b, g, :L] = new.astype(np.float32)
     return round_out(out, out_dtype), k_cache, v_cache, score, kind, orig_pos, length
+
+
+# --------------------------------------------------------------------------
+# drafted tokens: several entries at once, caches in pages
+# --------------------------------------------------------------------------
+# The paper decodes one token at a time from head-major caches; these definitions are this build's ("parity unpinned" by
+# the paper), pinned by brute force and by their agreement with decode_attn and prefill_attn.
+
+
+def slot_rows(pages, page_size: int, n_pages: int, Lmax: int, Hkv: int):
+    """place(b, g, slot) -> row of the cache seen as [rows, ...], or -1 (a page outside the pool).  pages None: head-major."""
+    def place(b, g, slot):
+        if pages is None:
+            return (b * Hkv + g) * Lmax + slot
+        page = int(pages[b, g, slot // page_size])
+        return page * page_size + slot % page_size if 0 <= page < n_pages else -1
+    return place
+
+
+def _where(k_cache, pages, Hkv):
+    if pages is None:
+        return slot_rows(None, 0, 0, k_cache.shape[2], Hkv), k_cache.shape[2]
+    n_pages, size = k_cache.shape[:2]
+    return slot_rows(pages, size, n_pages, pages.shape[2] * size, Hkv), pages.shape[2] * size
+
+
+def rotate(x, angles, adjacent: bool = False) -> np.ndarray:
+    """Pairs of the first 2 * len(angles) channels of x turned by their angles; the other channels stay."""
+    y = np.array(x, dtype=np.float64)
+    half = len(angles)
+    for c, a in enumerate(angles):
+        i, j = (2 * c, 2 * c + 1) if adjacent else (c, c + half)
+        y[..., i] = x[..., i] * math.cos(a) - x[..., j] * math.sin(a)
+        y[..., j] = x[..., j] * math.cos(a) + x[..., i] * math.sin(a)
+    return y
+
+
+def pair_angles(pos, inv_freq, sections):
+    """Angles of one token's pairs; pos: one position per axis, sections: pairs per axis in order."""
+    axis = [a for a, s in enumerate(sections) for _ in range(s)]
+    return [float(pos[a]) * float(f) for a, f in zip(axis, inv_freq)]
+
+
+def kv_append(k_new, v_new, k_cache, v_cache, length, *, pos=None, inv_freq=None, sections=None, adjacent=False, q=None, q_out=None,
+              n_new=None, pages=None, score=None, kind=None, orig_pos=None, new_kind=2, score_new=None, kind_new=None, orig_new=None):
+    """Returns (k_cache, v_cache, score, kind, orig_pos, length, q_out) after the append, in float64 / unrounded."""
+    B, T, Hkv, d = k_new.shape
+    place, Lmax = _where(k_cache, pages, Hkv)
+    out = [None if x is None else np.array(x) for x in (k_cache, v_cache, score, kind, orig_pos)]
+    flat = [None if x is None else x.reshape(-1, d) if i < 2 else x.reshape(-1) for i, x in enumerate(out)]
+    new_len = np.array(length)
+    turned = None if q_out is None else np.array(q_out, dtype=np.float64)
+    if pos is not None and pos.ndim == 2:
+        pos = pos[None]
+    if inv_freq is not None and sections is None:
+        sections = [len(inv_freq)]
+
+    def of(x, b, g, t):
+        return x[b, t] if x.ndim == 2 else x[b, g, t]
+
+    for b in range(B):
+        for g in range(Hkv):
+            n = T if n_new is None else int(n_new[b] if np.ndim(n_new) == 1 else n_new[b, g])
+            n = min(max(n, 0), T)
+            L = int(length[b, g])
+            if L < 0 or L + n > Lmax:
+                continue
+            for t in range(n):
+                row = place(b, g, L + t)
+                if row < 0:
+                    continue
+                flat[0][row] = k_new[b, t, g] if inv_freq is None else rotate(k_new[b, t, g], pair_angles(pos[:, b, t], inv_freq, sections), adjacent)
+                flat[1][row] = v_new[b, t, g]
+                if score is not None:
+                    flat[2][row] = 0.0 if score_new is None else of(score_new, b, g, t)
+                if kind is not None:
+                    flat[3][row] = new_kind if kind_new is None else of(kind_new, b, g, t)
+                if orig_pos is not None:
+                    flat[4][row] = of(orig_new, b, g, t) if orig_new is not None else pos[0, b, t] if pos is not None else t
+            new_len[b, g] = L + n
+        if q is not None:
+            n = T if n_new is None else min(max(int(n_new[b]), 0), T)
+            for t in range(n):
+                turned[b, t] = rotate(q[b, t], pair_angles(pos[:, b, t], inv_freq, sections), adjacent)
+    return (*out, new_len, turned)
+
+
+def tree_mask(parent) -> np.ndarray:
+    """Parents [T] (-1: a root) -> bool [T, T]: row t sees itself and its ancestors."""
+    T = len(parent)
+    sees = np.zeros((T, T), dtype=bool)
+    for t in range(T):
+        i = t
+        while i >= 0:
+            sees[t, i] = True
+            i = int(parent[i])
+    return sees
+
+
+def tree_attn(q, k_cache, v_cache, length, *, mask=None, n_rows=None, pages=None, scale=None, len_bound=0):
+    """q [B,T,Hq,d]; mask bool [B,T,T] (None: a chain) -> out [B,T,Hq,d], row_lse [B,Hq,T], sum of p |v| (for tolerances).
+    Rows from n_rows on are NaN in all three."""
+    B, T, Hq, d = q.shape
+    Hkv = length.shape[1]
+    G = Hq // Hkv
+    place, Lmax = _where(k_cache, pages, Hkv)
+    kf, vf = k_cache.reshape(-1, d), v_cache.reshape(-1, d)
+    scale = d ** -0.5 if scale is None else scale
+    out, weight = np.full((2, B, T, Hq, d), np.nan)
+    lse = np.full((B, Hq, T), np.nan)
+    for b in range(B):
+        n = T if n_rows is None else min(max(int(n_rows[b]), 0), T)
+        for g in range(Hkv):
+            L = int(length[b, g])
+            first = L - n
+            slots = range(max(0, min(L, len_bound or Lmax)))
+            rows = np.array([place(b, g, s) for s in slots], dtype=np.int64)
+            for t in range(n):
+                sees = np.array([r >= 0 and (s < first or (s - first <= t if mask is None else bool(mask[b, t, s - first])))
+                                 for s, r in zip(slots, rows)], dtype=bool)
+                at = rows[sees] if len(rows) else rows
+                for h in range(g * G, g * G + G):
+                    if len(at) == 0:
+                        out[b, t, h], weight[b, t, h], lse[b, h, t] = 0.0, 0.0, -np.inf
+                        continue
+                    z = scale * (kf[at] @ q[b, t, h])
+                    top = z.max()
+                    e = np.exp(z - top)
+                    lse[b, h, t] = top + np.log(e.sum())
+                    p = e / e.sum()
+                    out[b, t, h], weight[b, t, h] = p @ vf[at], p @ np.abs(vf[at])
+    return out, lse, weight
+
+
+def tree_commit(k_cache, v_cache, length, path, n_path, *, pages=None, score=None, kind=None, orig_pos=None):
+    """Returns (k_cache, v_cache, score, kind, orig_pos, length) with the accepted rows moved together."""
+    B, Hkv = length.shape
+    d = k_cache.shape[-1]
+    place, Lmax = _where(k_cache, pages, Hkv)
+    out = [None if x is None else np.array(x) for x in (k_cache, v_cache, score, kind, orig_pos)]
+    flat = [None if x is None else x.reshape(-1, d) if i < 2 else x.reshape(-1) for i, x in enumerate(out)]
+    new_len = np.array(length)
+    for b in range(B):
+        for g in range(Hkv):
+            L = int(length[b, g])
+            n = min(max(int(n_path[b]), 0), path.shape[1]) if L >= 0 else 0
+            before = -1
+            for i in range(n):
+                p = int(path[b, i])
+                if p <= before or L + p >= Lmax:
+                    break
+                before = p
+                src, dst = place(b, g, L + p), place(b, g, L + i)
+                if src >= 0 and dst >= 0:
+                    for x in flat:
+                        if x is not None:
+                            x[dst] = x[src]
+                new_len[b, g] = L + i + 1
+    return (*out, new_len)

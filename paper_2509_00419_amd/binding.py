@@ -24,6 +24,7 @@ TORCH_BINDING_PATH = os.environ.get("LVLM_TORCH_BINDING")       # ... and of the
 # ---- enums (include/lvlm.h) ----
 BF16, F32, I32 = 0, 1, 2
 OP_SCORE, OP_MERGE, OP_KV_COMPRESS, OP_DECODE_ATTN, OP_MERGE_SIMILAR, OP_SCORE_PROBS, OP_PREFILL_ATTN = 0, 1, 2, 3, 4, 5, 6
+OP_TREE_ATTN = 7
 MERGE_LINEAR_RANK, MERGE_PAIRWISE, MERGE_LINEAR_RAW = 0, 1, 2
 RULE_WEIGHTED, RULE_TOP = 0, 1
 KV_THRESHOLD, KV_BUDGET = 0, 1
@@ -91,6 +92,39 @@ class AttnDesc(C.Structure):
                 ("evict_budget", C.c_int32), ("evict_recent", C.c_int32)]
 
 
+class Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("score", C.c_void_p), ("kind", C.c_void_p), ("orig_pos", C.c_void_p),
+                ("pages", C.c_void_p), ("Lmax", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
+class AppendDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("B", C.c_int32), ("T", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32),
+                ("hd", C.c_int32), ("rot_dim", C.c_int32), ("adjacent", C.c_int32), ("n_axes", C.c_int32),
+                ("sections", C.c_int32 * 3), ("new_kind", C.c_int32), ("reserved", C.c_int32),
+                ("k_stride_b", C.c_int64), ("k_stride_t", C.c_int64), ("k_stride_h", C.c_int64),
+                ("v_stride_b", C.c_int64), ("v_stride_t", C.c_int64), ("v_stride_h", C.c_int64),
+                ("q_stride_b", C.c_int64), ("q_stride_t", C.c_int64), ("q_stride_h", C.c_int64),
+                ("qo_stride_b", C.c_int64), ("qo_stride_t", C.c_int64), ("qo_stride_h", C.c_int64),
+                ("n_stride_b", C.c_int64), ("n_stride_h", C.c_int64), ("m_stride_b", C.c_int64), ("m_stride_h", C.c_int64)]
+
+
+class AppendSrc(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("k", "v", "q", "q_out", "pos", "inv_freq", "n_new", "score", "kind", "orig_pos")]
+
+
+class TreeDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("B", C.c_int32), ("T", C.c_int32), ("Hq", C.c_int32), ("Hkv", C.c_int32),
+                ("hd", C.c_int32), ("Lmax", C.c_int32), ("len_bound", C.c_int32), ("scale", C.c_float), ("reserved", C.c_int32),
+                ("q_stride_b", C.c_int64), ("q_stride_t", C.c_int64), ("q_stride_h", C.c_int64),
+                ("o_stride_b", C.c_int64), ("o_stride_t", C.c_int64), ("o_stride_h", C.c_int64)]
+
+
+class CommitDesc(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("B", C.c_int32), ("Hkv", C.c_int32), ("hd", C.c_int32), ("P", C.c_int32),
+                ("reserved", C.c_int32)]
+
+
 class ProfileEntry(C.Structure):
     _fields_ = [("name", C.c_char * 48), ("calls", C.c_int32), ("total_ms", C.c_float), ("min_ms", C.c_float),
                 ("max_ms", C.c_float)]
@@ -128,6 +162,10 @@ def _load():
     lib.lvlm_decode_attn.argtypes = [vp, vp, C.POINTER(AttnDesc), vp, vp, vp, vp, vp, f32p, vp, i32p, i32p, vp]
     lib.lvlm_decode_attn_static.argtypes = lib.lvlm_decode_attn.argtypes
     lib.lvlm_decode_plan.argtypes = [vp, C.POINTER(AttnDesc), C.POINTER(C.c_int32), C.POINTER(C.c_int32), C.POINTER(C.c_int32)]
+    lib.lvlm_kv_append.argtypes = [vp, vp, C.POINTER(AppendDesc), C.POINTER(AppendSrc), C.POINTER(Cache), i32p, i32p]
+    lib.lvlm_tree_attn.argtypes = [vp, vp, C.POINTER(TreeDesc), vp, C.POINTER(Cache), i32p, i32p, i32p, vp, f32p]
+    lib.lvlm_tree_commit.argtypes = [vp, vp, C.POINTER(CommitDesc), C.POINTER(Cache), i32p, i32p, i32p, i32p]
+    lib.lvlm_tree_mask.argtypes = [C.c_int, C.c_void_p, C.c_void_p]
     lib.lvlm_stream_probe.argtypes = [vp, vp, vp, C.c_size_t, C.c_int32, vp]
     lib.lvlm_profile.argtypes = [C.c_void_p, C.c_int]
     lib.lvlm_profile_read.argtypes = [C.c_void_p, C.POINTER(ProfileEntry), C.c_int, C.POINTER(C.c_int)]
@@ -135,7 +173,8 @@ def _load():
                  "lvlm_merge_weights", "lvlm_score_tokens", "lvlm_score_plan", "lvlm_score_few_rows", "lvlm_score_shares", "lvlm_score_from_probs", "lvlm_prefill_attn", "lvlm_merge_compact",
                  "lvlm_merge_similar",
                  "lvlm_kv_compress",
-                 "lvlm_decode_attn", "lvlm_decode_attn_static", "lvlm_decode_plan", "lvlm_stream_probe"):
+                 "lvlm_decode_attn", "lvlm_decode_attn_static", "lvlm_decode_plan", "lvlm_kv_append", "lvlm_tree_attn",
+                 "lvlm_tree_commit", "lvlm_tree_mask", "lvlm_stream_probe"):
         getattr(lib, name).restype = C.c_int
     return lib
 
@@ -157,7 +196,7 @@ def _load_calls():
     address = lambda name: C.cast(getattr(lib, name), C.c_void_p).value          # noqa: E731
     _torch_binding.setup(LvlmError, *(address("lvlm_" + n) for n in (
         "last_error", "workspace_bytes", "set_workspace", "score_tokens", "score_from_probs", "prefill_attn", "merge_compact",
-        "merge_similar", "kv_compress", "decode_attn", "decode_attn_static")))
+        "merge_similar", "kv_compress", "decode_attn", "decode_attn_static", "kv_append", "tree_attn", "tree_commit")))
     return _torch_binding.ContextCalls
 
 
@@ -186,6 +225,21 @@ def merge_weights(mode: int, m: int) -> torch.Tensor:
     if st:
         raise LvlmError(st, "lvlm_merge_weights")
     return torch.tensor(list(out), dtype=torch.float32)
+
+
+def tree_mask(parent: torch.Tensor) -> torch.Tensor:
+    """lvlm_tree_mask: parents [T] or [B, T] (row before each row on its path, -1: a root) -> visibility words
+    [.., T, ceil(T / 32)] int32.  Host arithmetic: the parents are taken to the host, the words come back to their device."""
+    if parent.dim() not in (1, 2) or parent.shape[-1] < 1 or parent.dtype not in (torch.int32, torch.int64):
+        raise ValueError("parents are whole numbers, [T] or [B, T], T >= 1")
+    p = parent.detach().to("cpu").clamp(-2, 1024).to(torch.int32).contiguous()
+    T = p.shape[-1]
+    out = torch.empty(*p.shape, (T + 31) // 32, dtype=torch.int32)
+    for row, words in zip(p.view(-1, T), out.view(-1, T, out.shape[-1])):
+        st = lib.lvlm_tree_mask(T, row.data_ptr(), words.data_ptr())
+        if st:
+            raise LvlmError(st, "lvlm_tree_mask: at most 1024 rows, each parent in [-1, row)")
+    return out.to(parent.device)
 
 
 class Context(_ContextCalls):
@@ -241,8 +295,8 @@ class Context(_ContextCalls):
         return {arr[i].name.decode(): (arr[i].calls, arr[i].total_ms, arr[i].min_ms, arr[i].max_ms)
                 for i in range(n.value)}
 
-    # score_tokens, score_from_probs, prefill_attn, merge_compact, merge_similar, kv_compress and decode_attn are
-    # native (csrc/torch_binding.cpp), with the argument names and defaults that help(Context) shows.
+    # score_tokens, score_from_probs, prefill_attn, merge_compact, merge_similar, kv_compress, decode_attn, kv_append,
+    # tree_attn and tree_commit are native (csrc/torch_binding.cpp), with the argument names and defaults that help(Context) shows.
 
     # ---- step 1 ----
     def score_desc(self, q, k, *, q_pos0, img_begin, n_img, scale=None, causal=True, score_head=None) -> ScoreDesc:

@@ -157,6 +157,151 @@ const char *check_attn(const lvlm_attn_desc *d) {
     return nullptr;
 }
 
+// The cache of the drafted-token calls: its fields against each other (the pointers are looked at by the calls).
+const char *check_cache(const lvlm_cache *c) {
+    if (!c) return "null cache";
+    if (!c->k || !c->v) return "null pointer in the cache";
+    if (!aligned16(c->k) || !aligned16(c->v) || !aligned16(c->score) || !aligned16(c->kind) || !aligned16(c->orig_pos) ||
+        !aligned4(c->pages))
+        return "the cache's pointers must be 16-byte aligned (pages: 4)";
+    if (c->reserved != 0) return "reserved fields must be 0";
+    if (c->Lmax < 1) return "sizes must be positive";
+    if (c->Lmax > kMaxSlots) return kTooLarge;
+    if (!c->pages) return c->page_size != 0 || c->n_pages != 0 ? "page_size and n_pages need pages" : nullptr;
+    if (c->page_size < 16 || c->page_size > 65536 || (c->page_size & (c->page_size - 1)) != 0)
+        return "page_size must be a power of two, 16 to 65536";
+    if (c->Lmax % c->page_size != 0) return "Lmax must be a multiple of page_size";
+    if (c->n_pages < 1) return "n_pages must be positive";
+    return nullptr;
+}
+size_t cache_bytes(const lvlm_cache &c, int B, int Hkv, size_t row) {
+    return (c.pages ? (size_t)c.n_pages * c.page_size : (size_t)B * Hkv * c.Lmax) * row;
+}
+bool overlap(const void *p, size_t n, const void *q, size_t m) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(p), y = reinterpret_cast<uintptr_t>(q);
+    return n > 0 && m > 0 && x < y + m && y < x + n;
+}
+// Bytes from the first to behind the last element of x[b][t][h][0..hd).
+size_t span(int B, int T, int H, int hd, long long sb, long long st, long long sh, int eb) {
+    return (size_t)((B - 1) * sb + (T - 1) * st + (H - 1) * sh + hd) * eb;
+}
+constexpr long long kMaxStride = 1ll << 36;     // times any size, and the element size, within 63 bits
+// Strides of rows x[b][t][h]: whole vectors; no two rows of an output share elements.
+const char *check_rows(int B, int T, int H, int hd, long long sb, long long st, long long sh, int vec, bool written) {
+    if (sb < 0 || st < 0 || sh < 0 || sb % vec != 0 || st % vec != 0 || sh % vec != 0)
+        return "strides must be non-negative multiples of 16 bytes";
+    if (sb > kMaxStride || st > kMaxStride || sh > kMaxStride) return "strides beyond 2^36 elements";
+    if (!written) return nullptr;
+    // the axes in order of their strides, each beyond the span of the ones inside it
+    long long str[3] = {sb, st, sh}, cnt[3] = {B, T, H}, inside = hd;
+    for (int i = 0; i < 3; ++i)
+        for (int j = 0; j + 1 < 3; ++j)
+            if (str[j] > str[j + 1]) {
+                const long long s = str[j], c = cnt[j];
+                str[j] = str[j + 1]; str[j + 1] = s;
+                cnt[j] = cnt[j + 1]; cnt[j + 1] = c;
+            }
+    for (int i = 0; i < 3; ++i) {
+        if (cnt[i] <= 1) continue;
+        if (str[i] < inside) return "rows of an output overlap";
+        inside = (cnt[i] - 1) * str[i] + inside;
+    }
+    return nullptr;
+}
+
+const char *check_append(const lvlm_append_desc *d, const lvlm_append_src *s, const lvlm_cache *c) {
+    if (!d || !s) return "null descriptor";
+    if (!float_dtype(d->dtype)) return "dtype must be LVLM_BF16 or LVLM_F32";
+    if (d->hd != 64 && d->hd != 128) return "head dimension must be 64 or 128";
+    if (d->reserved != 0) return "reserved fields must be 0";
+    if (d->B < 1 || d->T < 0 || d->Hkv < 1 || (s->q && d->Hq < 1)) return "sizes must be positive";
+    if (d->B > kMaxBatch - 1 || d->T > kMaxTokens || d->Hkv > kMaxHeads || (s->q && d->Hq > kMaxHeads)) return kTooLarge;
+    if (d->rot_dim < 0 || d->rot_dim > d->hd || d->rot_dim % 16 != 0) return "rot_dim must be a multiple of 16 in [0, hd]";
+    if (d->adjacent != 0 && d->adjacent != 1) return "adjacent must be 0 or 1";
+    if (d->new_kind < 0 || d->new_kind > 255) return "new_kind out of range";
+    if (const char *why = check_cache(c)) return why;
+    if (d->T > 0 && (!s->k || !s->v)) return "null pointer";
+    if ((s->q == nullptr) != (s->q_out == nullptr)) return "q and q_out must be given together";
+    if (s->q && d->rot_dim == 0) return "q is only passed to be turned (rot_dim > 0)";
+    if (s->q && s->n_new && d->n_stride_h != 0) return "q needs counts per sequence (n_stride_h 0)";
+    if (d->rot_dim > 0) {
+        if (!s->pos || !s->inv_freq) return "pos and inv_freq are needed to turn";
+        if (d->n_axes < 1 || d->n_axes > 3) return "n_axes must be 1, 2 or 3";
+        long long sum = 0;
+        for (int i = 0; i < d->n_axes; ++i) {
+            if (d->sections[i] < 0) return "sections must not be negative";
+            sum += d->sections[i];
+        }
+        if (sum != d->rot_dim / 2) return "sections must add up to rot_dim / 2";
+    }
+    if (!aligned16(s->k) || !aligned16(s->v) || !aligned16(s->q) || !aligned16(s->q_out) || !aligned16(s->inv_freq))
+        return "k, v, q, q_out and inv_freq must be 16-byte aligned";
+    if (!aligned4(s->pos) || !aligned4(s->n_new) || !aligned4(s->score) || !aligned4(s->orig_pos))
+        return "pos, n_new, score and orig_pos must be 4-byte aligned";
+    if (d->n_stride_b < 0 || d->n_stride_h < 0 || d->m_stride_b < 0 || d->m_stride_h < 0) return "strides must not be negative";
+    if (d->n_stride_b > kMaxStride || d->n_stride_h > kMaxStride || d->m_stride_b > kMaxStride || d->m_stride_h > kMaxStride)
+        return "strides beyond 2^36 elements";
+    const int eb = elem_bytes(d->dtype), vec = 16 / eb, T = d->T > 0 ? d->T : 1;
+    const char *why;
+    if ((why = check_rows(d->B, T, d->Hkv, d->hd, d->k_stride_b, d->k_stride_t, d->k_stride_h, vec, false))) return why;
+    if ((why = check_rows(d->B, T, d->Hkv, d->hd, d->v_stride_b, d->v_stride_t, d->v_stride_h, vec, false))) return why;
+    const size_t cb = cache_bytes(*c, d->B, d->Hkv, (size_t)d->hd * eb);
+    const size_t kb = span(d->B, T, d->Hkv, d->hd, d->k_stride_b, d->k_stride_t, d->k_stride_h, eb);
+    const size_t vb = span(d->B, T, d->Hkv, d->hd, d->v_stride_b, d->v_stride_t, d->v_stride_h, eb);
+    if (overlap(s->k, kb, c->k, cb) || overlap(s->k, kb, c->v, cb) || overlap(s->v, vb, c->k, cb) || overlap(s->v, vb, c->v, cb))
+        return "new rows overlap the cache";
+    if (overlap(c->k, cb, c->v, cb)) return "the cache's keys and values overlap";
+    if (s->q) {
+        if ((why = check_rows(d->B, T, d->Hq, d->hd, d->q_stride_b, d->q_stride_t, d->q_stride_h, vec, false))) return why;
+        if ((why = check_rows(d->B, T, d->Hq, d->hd, d->qo_stride_b, d->qo_stride_t, d->qo_stride_h, vec, true))) return why;
+        const size_t qb = span(d->B, T, d->Hq, d->hd, d->q_stride_b, d->q_stride_t, d->q_stride_h, eb);
+        const size_t ob = span(d->B, T, d->Hq, d->hd, d->qo_stride_b, d->qo_stride_t, d->qo_stride_h, eb);
+        const bool same = s->q == s->q_out && d->q_stride_b == d->qo_stride_b && d->q_stride_t == d->qo_stride_t &&
+                          d->q_stride_h == d->qo_stride_h;
+        if (!same && overlap(s->q, qb, s->q_out, ob)) return "q_out overlaps q (it may only be q itself)";
+        if (overlap(s->q, qb, c->k, cb) || overlap(s->q, qb, c->v, cb) || overlap(s->q_out, ob, c->k, cb) ||
+            overlap(s->q_out, ob, c->v, cb))
+            return "q or q_out overlaps the cache";
+    }
+    return nullptr;
+}
+
+const char *check_tree(const lvlm_tree_desc *d) {
+    if (!d) return "null descriptor";
+    if (!float_dtype(d->dtype)) return "dtype must be LVLM_BF16 or LVLM_F32";
+    if (d->hd != 64 && d->hd != 128) return "head dimension must be 64 or 128";
+    if (d->reserved != 0) return "reserved fields must be 0";
+    if (d->B < 1 || d->Hq < 1 || d->Hkv < 1 || d->Lmax < 1) return "sizes must be positive";
+    if (d->B > kMaxBatch - 1 || d->Hq > kMaxHeads || d->Lmax > kMaxSlots) return kTooLarge;
+    if (d->Hq % d->Hkv != 0) return "Hq must be a multiple of Hkv";
+    if (d->T < 1 || d->T > 1024) return "T must be in [1, 1024]";
+    if ((long long)(d->Hq / d->Hkv) * d->T >= 65536) return "query rows per KV head (Hq/Hkv * T) must be below 65536";
+    if (d->len_bound < 0 || d->len_bound > d->Lmax) return "len_bound must be in [0, Lmax]";
+    if (!(d->scale > 0.0f) || !(d->scale < INFINITY)) return "scale must be positive and finite";
+    const int vec = 16 / elem_bytes(d->dtype);
+    if (const char *why = check_rows(d->B, d->T, d->Hq, d->hd, d->q_stride_b, d->q_stride_t, d->q_stride_h, vec, false)) return why;
+    return check_rows(d->B, d->T, d->Hq, d->hd, d->o_stride_b, d->o_stride_t, d->o_stride_h, vec, true);
+}
+
+const char *check_commit(const lvlm_commit_desc *d) {
+    if (!d) return "null descriptor";
+    if (!float_dtype(d->dtype)) return "dtype must be LVLM_BF16 or LVLM_F32";
+    if (d->hd != 64 && d->hd != 128) return "head dimension must be 64 or 128";
+    if (d->reserved != 0) return "reserved fields must be 0";
+    if (d->B < 1 || d->Hkv < 1) return "sizes must be positive";
+    if (d->B > kMaxBatch - 1 || d->Hkv > kMaxHeads) return kTooLarge;
+    if (d->P < 1 || d->P > 65536) return "P must be in [1, 65536]";
+    return nullptr;
+}
+
+// Lengths in and out: the same array, or two that do not touch.
+const char *check_lengths(const int32_t *len, const int32_t *len_out, int B, int Hkv) {
+    if (!len || !len_out) return "null pointer";
+    if (!aligned4(len) || !aligned4(len_out)) return "lengths must be 4-byte aligned";
+    const size_t n = (size_t)B * Hkv * 4;
+    return len != len_out && overlap(len, n, len_out, n) ? "len_out overlaps len (it may only be len itself)" : nullptr;
+}
+
 lvlm_status need_ws(lvlm_ctx *ctx, size_t bytes) {
     if (bytes == 0) return LVLM_OK;
     if (!ctx->ws) return fail(ctx, LVLM_ERR_WORKSPACE, "no workspace attached (need %zu bytes)", bytes);
@@ -175,6 +320,22 @@ lvlm_status bind_device(lvlm_ctx *ctx) {
     if (e != hipSuccess) return fail(ctx, LVLM_ERR_HIP, "hipSetDevice(%d): %s", ctx->device, hipGetErrorString(e));
     return LVLM_OK;
 }
+
+// The context's device for the length of a call; the caller's current one is put back.
+struct DeviceScope {
+    int before = -1, device;
+    hipError_t err;
+    explicit DeviceScope(const lvlm_ctx *ctx) : device(ctx->device) {
+        err = hipGetDevice(&before);
+        if (err == hipSuccess && before != device) err = hipSetDevice(device);
+    }
+    ~DeviceScope() {
+        if (before >= 0 && before != device) (void)hipSetDevice(before);
+    }
+    lvlm_status status(lvlm_ctx *ctx) const {
+        return err == hipSuccess ? LVLM_OK : fail(ctx, LVLM_ERR_HIP, "hipSetDevice(%d): %s", device, hipGetErrorString(err));
+    }
+};
 
 }  // namespace
 
@@ -282,6 +443,12 @@ lvlm_status lvlm_workspace_bytes(const lvlm_ctx *ctx, lvlm_op op, const void *de
             const auto *d = static_cast<const lvlm_prefill_desc *>(desc);
             if ((why = check_prefill(d))) break;
             *bytes = prefill_ws(*d).total;
+            return LVLM_OK;
+        }
+        case LVLM_OP_TREE_ATTN: {
+            const auto *d = static_cast<const lvlm_tree_desc *>(desc);
+            if ((why = check_tree(d))) break;
+            *bytes = tree_ws(*d).total;
             return LVLM_OK;
         }
         case LVLM_OP_MERGE:
@@ -529,6 +696,67 @@ static lvlm_status decode_attn_call(lvlm_ctx *ctx, bool static_scratch, void *st
     }
     return after_launch(ctx, launch_decode_attn(Prof{ctx, static_cast<hipStream_t>(stream)}, *d, w, ws,
                                                 q, k_new, v_new, k_cache, v_cache, score, kind, orig_pos, len, out));
+}
+
+lvlm_status lvlm_kv_append(lvlm_ctx *ctx, void *stream, const lvlm_append_desc *d, const lvlm_append_src *src,
+                           const lvlm_cache *cache, const int32_t *len, int32_t *len_out) {
+    if (!ctx) return LVLM_ERR_INVALID_ARG;
+    if (const char *why = check_append(d, src, cache)) return fail(ctx, LVLM_ERR_INVALID_ARG, "kv_append: %s", why);
+    if (const char *why = check_lengths(len, len_out, d->B, d->Hkv)) return fail(ctx, LVLM_ERR_INVALID_ARG, "kv_append: %s", why);
+    if (d->T == 0 && len == len_out) return LVLM_OK;
+    const DeviceScope scope(ctx);
+    if (lvlm_status st = scope.status(ctx)) return st;
+    return after_launch(ctx, launch_kv_append(Prof{ctx, static_cast<hipStream_t>(stream)}, *d, *src, *cache, len, len_out));
+}
+
+lvlm_status lvlm_tree_attn(lvlm_ctx *ctx, void *stream, const lvlm_tree_desc *d, const void *q, const lvlm_cache *cache,
+                           const int32_t *len, const int32_t *n_rows, const uint32_t *mask, void *out, float *row_lse) {
+    if (!ctx) return LVLM_ERR_INVALID_ARG;
+    if (const char *why = check_tree(d)) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: %s", why);
+    if (const char *why = check_cache(cache)) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: %s", why);
+    if (cache->Lmax != d->Lmax) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: Lmax of the descriptor and of the cache differ");
+    if (!q || !len || !out) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: null pointer");
+    if (!aligned16(q) || !aligned16(out)) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: q and out must be 16-byte aligned");
+    if (!aligned4(len) || !aligned4(n_rows) || !aligned4(mask) || !aligned4(row_lse))
+        return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: len, n_rows, mask and row_lse must be 4-byte aligned");
+    const int eb = elem_bytes(d->dtype);
+    const size_t qb = span(d->B, d->T, d->Hq, d->hd, d->q_stride_b, d->q_stride_t, d->q_stride_h, eb);
+    const size_t ob = span(d->B, d->T, d->Hq, d->hd, d->o_stride_b, d->o_stride_t, d->o_stride_h, eb);
+    const size_t cb = cache_bytes(*cache, d->B, d->Hkv, (size_t)d->hd * eb);
+    if (overlap(q, qb, out, ob) || overlap(cache->k, cb, out, ob) || overlap(cache->v, cb, out, ob))
+        return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: out overlaps q or the cache");
+    const TreeWs w = tree_ws(*d);
+    if (lvlm_status st = need_ws(ctx, w.total)) return st;
+    const DeviceScope scope(ctx);
+    if (lvlm_status st = scope.status(ctx)) return st;
+    return after_launch(ctx, launch_tree_attn(Prof{ctx, static_cast<hipStream_t>(stream)}, *d, w, static_cast<char *>(ctx->ws), q,
+                                              *cache, len, n_rows, mask, out, row_lse));
+}
+
+lvlm_status lvlm_tree_commit(lvlm_ctx *ctx, void *stream, const lvlm_commit_desc *d, const lvlm_cache *cache, const int32_t *len,
+                             const int32_t *path, const int32_t *n_path, int32_t *len_out) {
+    if (!ctx) return LVLM_ERR_INVALID_ARG;
+    if (const char *why = check_commit(d)) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_commit: %s", why);
+    if (const char *why = check_cache(cache)) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_commit: %s", why);
+    if (const char *why = check_lengths(len, len_out, d->B, d->Hkv)) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_commit: %s", why);
+    if (!path || !n_path) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_commit: null pointer");
+    if (!aligned4(path) || !aligned4(n_path)) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_commit: path and n_path must be 4-byte aligned");
+    const DeviceScope scope(ctx);
+    if (lvlm_status st = scope.status(ctx)) return st;
+    return after_launch(ctx, launch_tree_commit(Prof{ctx, static_cast<hipStream_t>(stream)}, *d, *cache, len, path, n_path, len_out));
+}
+
+lvlm_status lvlm_tree_mask(int T, const int32_t *parent, uint32_t *mask_out) {
+    if (T < 1 || T > 1024 || !parent || !mask_out) return LVLM_ERR_INVALID_ARG;
+    for (int t = 0; t < T; ++t)
+        if (parent[t] < -1 || parent[t] >= t) return LVLM_ERR_INVALID_ARG;
+    const int words = (T + 31) / 32;
+    for (int t = 0; t < T; ++t) {
+        uint32_t *row = mask_out + (size_t)t * words;
+        for (int w = 0; w < words; ++w) row[w] = parent[t] < 0 ? 0u : mask_out[(size_t)parent[t] * words + w];
+        row[t / 32] |= 1u << (t % 32);
+    }
+    return LVLM_OK;
 }
 
 lvlm_status lvlm_stream_probe(lvlm_ctx *ctx, void *stream, const void *src, size_t bytes, int32_t n_workgroups,

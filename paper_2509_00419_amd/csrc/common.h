@@ -159,6 +159,11 @@ struct AttnWs {
 };
 AttnWs attn_ws(const lvlm_attn_desc &d);
 
+struct TreeWs {
+    size_t total;
+};
+TreeWs tree_ws(const lvlm_tree_desc &d);
+
 // Names the kernel launches between begin() and end() for the optional timing.  The events are bound to the
 // kernels themselves (the start event to the first launch of the bracket, the stop event to its last), so what
 // is read back is the time from that kernel's first wave to its last -- the duration a kernel trace reports --
@@ -263,6 +268,13 @@ hipError_t launch_decode_attn(const Prof &prof, const lvlm_attn_desc &d, const A
                               const void *q, const void *k_new, const void *v_new, void *k_cache,
                               void *v_cache, float *score, uint8_t *kind, int32_t *orig_pos,
                               int32_t *len, void *out);
+
+hipError_t launch_kv_append(const Prof &prof, const lvlm_append_desc &d, const lvlm_append_src &s, const lvlm_cache &c,
+                            const int32_t *len, int32_t *len_out);
+hipError_t launch_tree_attn(const Prof &prof, const lvlm_tree_desc &d, const TreeWs &w, char *ws, const void *q, const lvlm_cache &c,
+                            const int32_t *len, const int32_t *n_rows, const uint32_t *mask, void *out, float *row_lse);
+hipError_t launch_tree_commit(const Prof &prof, const lvlm_commit_desc &d, const lvlm_cache &c, const int32_t *len,
+                              const int32_t *path, const int32_t *n_path, int32_t *len_out);
 
 hipError_t launch_stream_probe(const Prof &prof, const void *src, size_t bytes, int n_workgroups, unsigned int *sink);
 

@@ -33,6 +33,9 @@ struct Lib {
     decltype(&lvlm_kv_compress) kv_compress;
     decltype(&lvlm_decode_attn) decode_attn;
     decltype(&lvlm_decode_attn_static) decode_attn_static;
+    decltype(&lvlm_kv_append) kv_append;
+    decltype(&lvlm_tree_attn) tree_attn;
+    decltype(&lvlm_tree_commit) tree_commit;
 } lib;
 PyObject *lvlm_error = nullptr;
 
@@ -507,6 +510,230 @@ PyObject *decode_attn(Core *c, PyObject *const *a) {
     return out.take();
 }
 
+// ---- drafted tokens ----
+// The calls below go to the context's device, on that device's current stream, whichever device is current.
+void *stream_of(Core *c) {
+    return static_cast<void *>(c10::hip::getCurrentHIPStream((c10::DeviceIndex)c->device).stream());
+}
+// A tensor on the context's device, of one type.
+const at::Tensor &here(Core *c, PyObject *o, const char *what, at::ScalarType dt) {
+    const at::Tensor &t = tensor(o, what);
+    if (!t.is_cuda() || t.get_device() != c->device) {
+        PyErr_Format(PyExc_AssertionError, "%s must be on the context's device, cuda:%d", what, c->device);
+        throw PyErr{};
+    }
+    if (t.scalar_type() != dt) {
+        PyErr_Format(PyExc_AssertionError, "%s must be %s", what, c10::toString(dt));
+        throw PyErr{};
+    }
+    return t;
+}
+// ... contiguous, of the given sizes
+const at::Tensor &dense(Core *c, PyObject *o, const char *what, at::ScalarType dt, at::IntArrayRef sizes) {
+    const at::Tensor &t = here(c, o, what, dt);
+    if (t.sizes() != sizes || !t.is_contiguous()) {
+        PyErr_Format(PyExc_AssertionError, "%s must be contiguous, of the sizes the other arguments give", what);
+        throw PyErr{};
+    }
+    return t;
+}
+// the stride of an axis; 0 where the axis has one place, whatever torch says there
+int64_t stride_of(const at::Tensor &t, int i) { return t.size(i) > 1 ? t.stride(i) : 0; }
+
+// The cache arguments: head-major [B, Hkv, Lmax, d], or [n_pages, page, d] with a table.
+lvlm_cache cache_of(Core *c, PyObject *ko, PyObject *vo, PyObject *pages, PyObject *score, PyObject *kind, PyObject *orig, int64_t B,
+                    int64_t Hkv, int64_t hd) {
+    const at::Tensor &k = tensor(ko, "k_cache"), &v = tensor(vo, "v_cache");
+    const at::ScalarType dt = k.scalar_type();
+    here(c, ko, "k_cache", dt);
+    dense(c, vo, "v_cache", dt, k.sizes());
+    require(k.is_contiguous(), "the caches must be contiguous");
+    lvlm_cache r{};
+    if (given(pages)) {
+        require(k.dim() == 3 && k.size(2) == hd, "with pages the caches must be [n_pages, page, d]");
+        const at::Tensor &p = here(c, pages, "pages", at::kInt);
+        require(p.dim() == 3 && p.size(0) == B && p.size(1) == Hkv && p.is_contiguous(), "pages must be [B, Hkv, max_pages], contiguous");
+        require(k.size(0) < (1ll << 31) && k.size(1) <= 65536 && p.size(2) * k.size(1) < (1ll << 31), "too many pages");
+        r.pages = (const int32_t *)p.data_ptr();
+        r.n_pages = (int32_t)k.size(0);
+        r.page_size = (int32_t)k.size(1);
+        r.Lmax = (int32_t)(p.size(2) * k.size(1));
+    } else {
+        require(k.dim() == 4 && k.size(0) == B && k.size(1) == Hkv && k.size(3) == hd, "the caches must be [B, Hkv, Lmax, d]");
+        require(k.size(2) < (1ll << 31), "too many slots");
+        r.Lmax = (int32_t)k.size(2);
+    }
+    r.k = k.data_ptr();
+    r.v = v.data_ptr();
+    const at::IntArrayRef slots = k.sizes().slice(0, k.dim() - 1);
+    if (given(score)) r.score = (float *)dense(c, score, "score", at::kFloat, slots).data_ptr();
+    if (given(kind)) r.kind = (uint8_t *)dense(c, kind, "kind", at::kByte, slots).data_ptr();
+    if (given(orig)) r.orig_pos = (int32_t *)dense(c, orig, "orig_pos", at::kInt, slots).data_ptr();
+    return r;
+}
+
+Signature sig_append{"kv_append", 5, 21, 0x1fu,
+                     {"k_new", "v_new", "k_cache", "v_cache", "length", "pos", "inv_freq", "sections", "adjacent", "q", "q_out",
+                      "n_new", "pages", "score", "kind", "orig_pos", "new_kind", "score_new", "kind_new", "orig_new", "length_out"}, {}};
+PyObject *kv_append(Core *c, PyObject *const *a) {
+    const at::Tensor &k = tensor(a[0], "k_new"), &v = tensor(a[1], "v_new");
+    const at::ScalarType dt = tensor(a[2], "k_cache").scalar_type();
+    dims(k, 4, "k_new must be [B, T, Hkv, d]");
+    here(c, a[0], "k_new", dt);
+    here(c, a[1], "v_new", dt);
+    require(v.sizes() == k.sizes(), "v_new must be [B, T, Hkv, d] as k_new");
+    const int64_t B = k.size(0), T = k.size(1), H = k.size(2), hd = k.size(3);
+    require(hd == 0 || (stride_of(k, 3) <= 1 && stride_of(v, 3) <= 1), "head dimension must be contiguous");
+    require(B < (1ll << 31) && T < (1ll << 31) && H < (1ll << 31) && hd < (1ll << 31), "too large");
+    lvlm_append_desc d{};
+    lvlm_append_src s{};
+    d.dtype = dtype_code(k);
+    d.B = (int32_t)B; d.T = (int32_t)T; d.Hkv = (int32_t)H; d.hd = (int32_t)hd;
+    d.k_stride_b = stride_of(k, 0); d.k_stride_t = stride_of(k, 1); d.k_stride_h = stride_of(k, 2);
+    d.v_stride_b = stride_of(v, 0); d.v_stride_t = stride_of(v, 1); d.v_stride_h = stride_of(v, 2);
+    s.k = k.data_ptr();
+    s.v = v.data_ptr();
+    const lvlm_cache cache = cache_of(c, a[2], a[3], a[12], a[13], a[14], a[15], B, H, hd);
+    const at::Tensor &len = dense(c, a[4], "length", at::kInt, {B, H});
+    require(given(a[5]) == given(a[6]), "pos and inv_freq must be given together");
+    if (given(a[5])) {
+        const at::Tensor &pos = here(c, a[5], "pos", at::kInt), &freq = here(c, a[6], "inv_freq", at::kFloat);
+        require(freq.dim() == 1 && freq.is_contiguous() && freq.numel() <= 4096, "inv_freq must be [pairs], contiguous");
+        d.rot_dim = (int32_t)(2 * freq.numel());
+        d.n_axes = 1;
+        d.sections[0] = d.rot_dim / 2;
+        if (given(a[7])) {
+            PyObject *f = PySequence_Fast(a[7], "sections must be a sequence");
+            if (!f) throw PyErr{};
+            struct Held { PyObject *o; ~Held() { Py_DECREF(o); } } held{f};
+            const Py_ssize_t n = PySequence_Fast_GET_SIZE(f);
+            require(n >= 1 && n <= 3, "sections: pairs of one to three axes");
+            d.n_axes = (int32_t)n;
+            for (Py_ssize_t i = 0; i < n; ++i) d.sections[i] = integer(PySequence_Fast_GET_ITEM(f, i), 0);
+        }
+        const bool flat = pos.dim() == 2 && d.n_axes == 1;
+        require(pos.is_contiguous() && (flat ? pos.size(0) == B && pos.size(1) == T
+                                             : pos.dim() == 3 && pos.size(0) == d.n_axes && pos.size(1) == B && pos.size(2) == T),
+                "pos must be [B, T], or [axes, B, T] with as many sections, contiguous");
+        s.pos = (const int32_t *)pos.data_ptr();
+        s.inv_freq = (const float *)freq.data_ptr();
+    } else {
+        require(!given(a[7]), "sections need pos and inv_freq");
+    }
+    d.adjacent = truth(a[8], false);
+    Out q_out, len_out;
+    require(given(a[9]) || !given(a[10]), "q_out needs q");
+    if (given(a[9])) {
+        const at::Tensor &q = here(c, a[9], "q", dt);
+        dims(q, 4, "q must be [B, T, Hq, d]");
+        require(q.size(0) == B && q.size(1) == T && q.size(3) == hd && q.size(2) < (1ll << 31), "q must be [B, T, Hq, d]");
+        if (!q_out.set(a[10])) q_out.set(empty(q.sizes(), q, dt));
+        const at::Tensor &o = here(c, q_out.o, "q_out", dt);
+        require(o.sizes() == q.sizes() && stride_of(q, 3) == 1 && stride_of(o, 3) == 1, "q_out must be [B, T, Hq, d]; head dimension contiguous");
+        d.Hq = (int32_t)q.size(2);
+        d.q_stride_b = stride_of(q, 0); d.q_stride_t = stride_of(q, 1); d.q_stride_h = stride_of(q, 2);
+        d.qo_stride_b = stride_of(o, 0); d.qo_stride_t = stride_of(o, 1); d.qo_stride_h = stride_of(o, 2);
+        if (q.numel() > 0) {
+            s.q = q.data_ptr();
+            s.q_out = o.data_ptr();
+        }
+    }
+    if (given(a[11])) {
+        const at::Tensor &n = here(c, a[11], "n_new", at::kInt);
+        require((n.dim() == 1 && n.size(0) == B) || (n.dim() == 2 && n.size(0) == B && n.size(1) == H), "n_new must be [B] or [B, Hkv]");
+        d.n_stride_b = stride_of(n, 0);
+        d.n_stride_h = n.dim() == 2 ? n.stride(1) : 0;
+        s.n_new = (const int32_t *)n.data_ptr();
+    }
+    d.new_kind = integer(a[16], LVLM_KIND_GENERATED);
+    bool first = true;
+    const auto per_entry = [&](PyObject *o, const char *what, at::ScalarType type) -> void * {
+        if (!given(o)) return nullptr;
+        const at::Tensor &t = here(c, o, what, type);
+        const bool shared = t.dim() == 2;
+        require(shared ? t.size(0) == B && t.size(1) == T : t.dim() == 3 && t.size(0) == B && t.size(1) == H && t.size(2) == T,
+                "score_new, kind_new and orig_new must be [B, T] or [B, Hkv, T]");
+        const int64_t sb = stride_of(t, 0), sh = shared ? 0 : stride_of(t, 1);
+        require(T <= 1 || stride_of(t, t.dim() - 1) == 1, "score_new, kind_new and orig_new need contiguous rows");
+        if (first) d.m_stride_b = sb, d.m_stride_h = sh;
+        require(first || (d.m_stride_b == sb && d.m_stride_h == sh), "score_new, kind_new and orig_new must have the same strides");
+        first = false;
+        return t.data_ptr();
+    };
+    s.score = (const float *)per_entry(a[17], "score_new", at::kFloat);
+    s.kind = (const uint8_t *)per_entry(a[18], "kind_new", at::kByte);
+    s.orig_pos = (const int32_t *)per_entry(a[19], "orig_new", at::kInt);
+    if (!len_out.set(a[20])) len_out.set(empty({B, H}, k, at::kInt));
+    const at::Tensor &lo = dense(c, len_out.o, "length_out", at::kInt, {B, H});
+    void *st = stream_of(c);
+    const int32_t *pl = (const int32_t *)len.data_ptr();
+    int32_t *po = (int32_t *)lo.data_ptr();
+    launch(c, [&] { return lib.kv_append(c->h, st, &d, &s, &cache, pl, po); });
+    return tuple_of(len_out, q_out);
+}
+
+Signature sig_tree{"tree_attn", 4, 13, 0xfu,
+                   {"q", "k_cache", "v_cache", "length", "mask", "n_rows", "pages", "scale", "len_bound", "out", "row_lse", "want_lse",
+                    "reserve"}, {}};
+PyObject *tree_attn(Core *c, PyObject *const *a) {
+    const at::Tensor &q = tensor(a[0], "q"), &len = tensor(a[3], "length");
+    const at::ScalarType dt = tensor(a[1], "k_cache").scalar_type();
+    here(c, a[0], "q", dt);
+    dims(q, 4, "q must be [B, T, Hq, d]");
+    dims(len, 2, "length must be [B, Hkv]");
+    const int64_t B = q.size(0), T = q.size(1), Hq = q.size(2), hd = q.size(3), H = len.size(1);
+    require(B < (1ll << 31) && T < (1ll << 31) && Hq < (1ll << 31) && hd < (1ll << 31) && H < (1ll << 31), "too large");
+    require(stride_of(q, 3) <= 1, "head dimension must be contiguous");
+    lvlm_tree_desc d{};
+    d.dtype = dtype_code(q);
+    d.B = (int32_t)B; d.T = (int32_t)T; d.Hq = (int32_t)Hq; d.Hkv = (int32_t)H; d.hd = (int32_t)hd;
+    const lvlm_cache cache = cache_of(c, a[1], a[2], a[6], nullptr, nullptr, nullptr, B, H, hd);
+    dense(c, a[3], "length", at::kInt, {B, H});
+    d.Lmax = cache.Lmax;
+    d.len_bound = integer(a[8], 0);
+    d.scale = (float)(given(a[7]) ? real(a[7]) : 1.0 / std::sqrt((double)hd));
+    const int32_t *rows = given(a[5]) ? (const int32_t *)dense(c, a[5], "n_rows", at::kInt, {B}).data_ptr() : nullptr;
+    const uint32_t *mask = given(a[4]) ? (const uint32_t *)dense(c, a[4], "mask", at::kInt, {B, T, (T + 31) / 32}).data_ptr() : nullptr;
+    Out out, lse;
+    if (!out.set(a[9])) out.set(empty(q.sizes(), q, dt));
+    if (!lse.set(a[10]) && truth(a[11], false)) lse.set(empty({B, Hq, T}, q, at::kFloat));
+    const at::Tensor &o = here(c, out.o, "out", dt);
+    require(o.sizes() == q.sizes() && stride_of(o, 3) <= 1, "out must be [B, T, Hq, d]; head dimension contiguous");
+    float *pl = lse.o ? (float *)dense(c, lse.o, "row_lse", at::kFloat, {B, Hq, T}).data_ptr() : nullptr;
+    d.q_stride_b = stride_of(q, 0); d.q_stride_t = stride_of(q, 1); d.q_stride_h = stride_of(q, 2);
+    d.o_stride_b = stride_of(o, 0); d.o_stride_t = stride_of(o, 1); d.o_stride_h = stride_of(o, 2);
+    if (truth(a[12], true)) reserve_for(c, LVLM_OP_TREE_ATTN, &d);
+    void *s = stream_of(c), *pq = q.data_ptr(), *po = o.data_ptr();
+    const int32_t *pn = (const int32_t *)len.data_ptr();
+    launch(c, [&] { return lib.tree_attn(c->h, s, &d, pq, &cache, pn, rows, mask, po, pl); });
+    return tuple_of(out, lse);
+}
+
+Signature sig_commit{"tree_commit", 5, 10, 0x1fu,
+                     {"k_cache", "v_cache", "length", "path", "n_path", "pages", "score", "kind", "orig_pos", "length_out"}, {}};
+PyObject *tree_commit(Core *c, PyObject *const *a) {
+    const at::Tensor &k = tensor(a[0], "k_cache"), &len = tensor(a[2], "length"), &path = tensor(a[3], "path");
+    dims(len, 2, "length must be [B, Hkv]");
+    dims(path, 2, "path must be [B, P]");
+    require(k.dim() >= 1, "the caches must be [B, Hkv, Lmax, d] or [n_pages, page, d]");
+    const int64_t B = len.size(0), H = len.size(1), hd = k.size(k.dim() - 1), P = path.size(1);
+    require(B < (1ll << 31) && H < (1ll << 31) && hd < (1ll << 31) && P < (1ll << 31), "too large");
+    const lvlm_cache cache = cache_of(c, a[0], a[1], a[5], a[6], a[7], a[8], B, H, hd);
+    dense(c, a[2], "length", at::kInt, {B, H});
+    lvlm_commit_desc d{};
+    d.dtype = dtype_code(k);
+    d.B = (int32_t)B; d.Hkv = (int32_t)H; d.hd = (int32_t)hd; d.P = (int32_t)P;
+    const int32_t *pp = (const int32_t *)dense(c, a[3], "path", at::kInt, {B, P}).data_ptr();
+    const int32_t *pn = (const int32_t *)dense(c, a[4], "n_path", at::kInt, {B}).data_ptr();
+    Out len_out;
+    if (!len_out.set(a[9])) len_out.set(empty({B, H}, len, at::kInt));
+    int32_t *po = (int32_t *)dense(c, len_out.o, "length_out", at::kInt, {B, H}).data_ptr();
+    void *s = stream_of(c);
+    const int32_t *pl = (const int32_t *)len.data_ptr();
+    launch(c, [&] { return lib.tree_commit(c->h, s, &d, &cache, pl, pp, pn, po); });
+    return len_out.take();
+}
+
 // ---- the type ----
 template <Signature &SIG, PyObject *(*IMPL)(Core *, PyObject *const *)>
 PyObject *entry(PyObject *self, PyObject *const *args, Py_ssize_t n_args, PyObject *kwnames) {
@@ -597,6 +824,25 @@ PyMethodDef methods[] = {
                 "static_scratch=False)\n--\n\n"
                 "lvlm_decode_attn.  q [B,Hq,d], k_new/v_new [B,Hkv,d] or None -> out [B,Hq,d].\n"
                 "static_scratch: lvlm_decode_attn_static instead (the library's own fixed scratch array, no workspace)."),
+    LVLM_METHOD(kv_append, sig_append,
+                "kv_append($self, k_new, v_new, k_cache, v_cache, length, *, pos=None, inv_freq=None, sections=None, adjacent=False, "
+                "q=None, q_out=None, n_new=None, pages=None, score=None, kind=None, orig_pos=None, new_kind=2, score_new=None, "
+                "kind_new=None, orig_new=None, length_out=None)\n--\n\n"
+                "lvlm_kv_append.  k_new, v_new [B,T,Hkv,d] into caches [B,Hkv,Lmax,d], or [n_pages,page,d] with pages\n"
+                "[B,Hkv,max_pages]; keys, and q [B,T,Hq,d], turned by pos ([B,T], or [axes,B,T] with sections: pairs per axis)\n"
+                "times inv_freq [pairs].  n_new [B] or [B,Hkv]; score_new, kind_new, orig_new [B,T] or [B,Hkv,T].\n"
+                "Returns (length_out [B,Hkv], q_out); length stays unless it is passed as length_out."),
+    LVLM_METHOD(tree_attn, sig_tree,
+                "tree_attn($self, q, k_cache, v_cache, length, *, mask=None, n_rows=None, pages=None, scale=None, len_bound=0, "
+                "out=None, row_lse=None, want_lse=False, reserve=True)\n--\n\n"
+                "lvlm_tree_attn.  q [B,T,Hq,d] over caches that hold the drafted rows as the last n_rows [B] (None: T) of their\n"
+                "length [B,Hkv] entries; mask [B,T,ceil(T/32)] int32 words (tree_mask; None: a chain).\n"
+                "Returns (out [B,T,Hq,d], row_lse [B,Hq,T] or None)."),
+    LVLM_METHOD(tree_commit, sig_commit,
+                "tree_commit($self, k_cache, v_cache, length, path, n_path, *, pages=None, score=None, kind=None, orig_pos=None, "
+                "length_out=None)\n--\n\n"
+                "lvlm_tree_commit (in place).  length [B,Hkv] before the drafts, path [B,P] ascending drafted rows, n_path [B];\n"
+                "returns length_out [B,Hkv] (length itself may be passed)."),
     {"reserve", reserve, METH_O, "reserve($self, nbytes, /)\n--\n\nGrows the attached workspace (never shrinks); call outside graph capture."},
     {"_attach", attach, METH_VARARGS, "The lvlm_ctx handle (an address, 0: none) and device the calls go to."},
     {nullptr, nullptr, 0, nullptr}};
@@ -607,8 +853,9 @@ PyTypeObject core_type = {PyVarObject_HEAD_INIT(nullptr, 0) "paper_2509_00419_am
 // setup(error class, address of lvlm_last_error, ... in the order of Lib)
 PyObject *setup(PyObject *, PyObject *args) {
     PyObject *err;
-    unsigned long long p[11];
-    if (!PyArg_ParseTuple(args, "OKKKKKKKKKKK", &err, &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9], &p[10]))
+    unsigned long long p[14];
+    if (!PyArg_ParseTuple(args, "OKKKKKKKKKKKKKK", &err, &p[0], &p[1], &p[2], &p[3], &p[4], &p[5], &p[6], &p[7], &p[8], &p[9], &p[10],
+                          &p[11], &p[12], &p[13]))
         return nullptr;
     Py_INCREF(err);
     Py_XSETREF(lvlm_error, err);
@@ -624,7 +871,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_binding", "Native calls of 
 }  // namespace
 
 PyMODINIT_FUNC PyInit__torch_binding(void) {
-    for (Signature *s : {&sig_score, &sig_probs, &sig_prefill, &sig_merge, &sig_similar, &sig_kv, &sig_decode}) s->intern();
+    for (Signature *s : {&sig_score, &sig_probs, &sig_prefill, &sig_merge, &sig_similar, &sig_kv, &sig_decode, &sig_append, &sig_tree, &sig_commit}) s->intern();
     core_type.tp_basicsize = sizeof(Core);
     core_type.tp_flags = Py_TPFLAGS_DEFAULT | Py_TPFLAGS_BASETYPE;
     core_type.tp_doc = "The per-call methods of binding.Context.";
