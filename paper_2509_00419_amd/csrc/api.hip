@@ -276,6 +276,7 @@ const char *check_tree(const lvlm_tree_desc *d) {
     if (d->Hq % d->Hkv != 0) return "Hq must be a multiple of Hkv";
     if (d->T < 1 || d->T > 1024) return "T must be in [1, 1024]";
     if ((long long)(d->Hq / d->Hkv) * d->T >= 65536) return "query rows per KV head (Hq/Hkv * T) must be below 65536";
+    if ((long long)d->B * d->Hq * d->T >= (1ll << 31)) return "query rows (B * Hq * T) must be below 2^31";
     if (d->len_bound < 0 || d->len_bound > d->Lmax) return "len_bound must be in [0, Lmax]";
     if (!(d->scale > 0.0f) || !(d->scale < INFINITY)) return "scale must be positive and finite";
     const int vec = 16 / elem_bytes(d->dtype);

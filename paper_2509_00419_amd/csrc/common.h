@@ -160,7 +160,9 @@ struct AttnWs {
 AttnWs attn_ws(const lvlm_attn_desc &d);
 
 struct TreeWs {
-    size_t total;
+    size_t part_o, part_ml, total;
+    int n_split, split_len;     // runs of a pair's entries (split_len each), folded by a second launch
+    int row_blocks;             // workgroups a pair's rows take
 };
 TreeWs tree_ws(const lvlm_tree_desc &d);
 
