@@ -44,7 +44,8 @@ __device__ __forceinline__ int rows_in_use(const TreeArgs &a, int b) {
     return a.n_rows ? min(max(uniform_word(a.n_rows + b), 0), a.T) : a.T;
 }
 
-constexpr float kLazyTree = 8.f;    // log2 of how far a row's maximum may run ahead of the reference before a rescale
+constexpr float kLazyTree = 8.f;    // careful tiles: log2 of how far a row's maximum may run ahead of the reference before a rescale
+constexpr float kRiskTree = 64.f;   // clear tiles: ... before the workgroup does its rows again with care
 
 template <int DT, int HD, int RB, int KW>
 struct TreeShape {
@@ -53,12 +54,21 @@ struct TreeShape {
     static constexpr int TILEB = 32 * ROWB;             // ... of a tile's keys (or values)
     static constexpr int RW = 4 / KW;                   // waves side by side over rows
     static constexpr int ROWS = 32 * RB * RW;           // rows of a workgroup
-    static constexpr int RING0 = (128 << 10) / (KW * 2 * TILEB);
-    static constexpr int RING = RING0 > 4 ? 4 : RING0;  // steps of KW tiles in LDS
+    static constexpr bool PIPED = DT == LVLM_BF16 && RB == 2;   // three tiles at different stages at a time
+    static constexpr int TPS = PIPED ? 2 : 1;           // tiles of a wave in a step
+    static constexpr int STEPB = KW * TPS * 2 * TILEB;
+    // Steps in LDS (piped: a step's keys are read a step before its values and travel a step ahead of them).  Two workgroups share a
+    // compute unit where two steps each leave room for it.
+    static constexpr int RING = PIPED ? (HD == 128 ? 4 : 8) : 2 * STEPB > (64 << 10) ? 2 : (64 << 10) / STEPB > 4 ? 4 : (64 << 10) / STEPB;
+    static constexpr int REACH = PIPED ? RING : RING - 1;       // the step that is fetched next (piped: of keys), from the one in hand
+    static constexpr int OPEN = PIPED ? RING - 3 : RW == 1 ? RING - 1 : RING - 2;       // steps still travelling when it is waited for
+    static constexpr int PER_CU = DT == LVLM_BF16 && !PIPED && RING * STEPB <= (64 << 10) ? 2 : 1;     // workgroups to a compute unit
     static constexpr int PITCH = HD * 4 + 16;           // of a row of sums put together in LDS
-    static constexpr int RING_BYTES = RING * KW * 2 * TILEB, MERGE_BYTES = 4 * 32 * PITCH;
-    static constexpr int LDS = RING_BYTES > MERGE_BYTES ? RING_BYTES : MERGE_BYTES;
-    static_assert(RING >= 2, "the next step's tiles travel while this one's are used");
+    static constexpr int P_PITCH = 34, P_BYTES = 4 * 32 * P_PITCH * 2;
+    static constexpr int RING_BYTES = RING * STEPB, MERGE_BYTES = 4 * 32 * PITCH;
+    static constexpr int LDS = RING_BYTES + P_BYTES > MERGE_BYTES ? RING_BYTES + P_BYTES : MERGE_BYTES;
+    static_assert(RING >= 2 && LDS + 1040 <= (160 << 10) / PER_CU, "the next step's tiles travel while this one's are used");
+    static_assert(KW == 1 || !PIPED, "the waves of a piped workgroup take the same tiles, and load keys or values");
     // a word of values (one, or two in bf16): is any of them NaN or infinite; the word with 0 in their place
     __device__ static __forceinline__ bool not_finite(uint32_t w) {
         return (w & 0x7f800000u) == 0x7f800000u || (DT == LVLM_BF16 && (w & 0x7f80u) == 0x7f80u);
@@ -70,21 +80,32 @@ struct TreeShape {
     }
 };
 
+__device__ __forceinline__ uint32_t pack_p(float lo, float hi) {
+    typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{lo, hi}, bf2));
+}
+
 // Four waves: KW of them share the entries tile by tile, 4 / KW the rows, RB blocks of 32 rows each.  Tiles of 32 entries go from
-// memory to LDS directly, RING steps of KW tiles ahead; a 16-byte unit lies at a place that depends on its row, so
+// memory to LDS directly, some steps of KW tiles ahead; a 16-byte unit lies at a place that depends on its row, so
 // that the 16 rows (keys) or 8 rows (values) that are read together lie in different banks.  The values are turned around on
 // their way out of LDS by its transposing read: lane l of 16 gets four entries of channel l, which is the order the
 // probabilities have in the accumulator registers of the first product.
+//
+// Clear tiles, which every row sees whole, take the maximum of a wave's first one as reference and never rescale; should a
+// sum rise beyond 2^kRiskTree, the workgroup does its rows again with care.  Careful tiles (drafts, the last ones, pages
+// outside the pool) are masked by words of 32 bits and rescale as the running maximum moves.
 template <int DT, int HD, int RB, int KW>
-__global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
+__global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree_attn_kernel(TreeArgs a) {
     using Z = TreeShape<DT, HD, RB, KW>;
     constexpr int ES = Z::ES, ROWB = Z::ROWB, TILEB = Z::TILEB, RW = Z::RW, RING = Z::RING;
-    constexpr int UPR = ROWB / 16, RPL = 1024 / ROWB;           // units per row; rows per load (1: half a row or more)
+    constexpr int UPR = ROWB / 16, RPL = 1024 / ROWB;           // units per row; rows per load
     constexpr int LOADS = 2 * TILEB / 1024, NL = LOADS / RW;    // loads of a tile, of a wave
-    constexpr int NV = HD * ES / 32, NCB = HD / 32;
+    constexpr int NV = HD * ES / 32, NCB = HD / 32, TPS = Z::TPS;
     __shared__ __attribute__((aligned(1024))) char lds[Z::LDS];
-    __shared__ __attribute__((aligned(16))) float p_s[4][32 * 33];
-    __shared__ float m_s[4][32 * RB], l_s[4][32 * RB];
+    __shared__ float m_s[4][32], l_s[4][32];
+    __shared__ int again_s[4];
+    char *const p_mem = lds + Z::RING_BYTES;
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -107,8 +128,9 @@ __global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
     if (s_lo >= s_hi && a.n_split > 1) return;
     const int first = max(len, 0) - n;              // entry of drafted row 0 (below 0: the head holds fewer than n)
     const int n_tiles = s_hi > s_lo ? (s_hi - s_lo + 31) >> 5 : 0;
-    const int n_steps = (n_tiles + KW - 1) / KW;
-    const int clear_to = min(min(first, L), s_hi);  // tiles up to here are seen whole by every row
+    const int n_steps = (n_tiles + KW * TPS - 1) / (KW * TPS);
+    // leading tiles that every row sees whole (fewer once one in no page turns up)
+    int n_clear = max(min(min(first, L), s_hi) - s_lo, 0) >> 5;
 
     // ---- moving the entries
     auto place_k = [](int row) { return ROWB == 128 ? (row >> 1) & 7 : row & 15; };
@@ -129,56 +151,79 @@ __global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
             const int row = RPL * y + lane / UPR;
             off[p][y] = row * ROWB + unit_of(row, SETS == 2 ? p == 0 : rw * NL < LOADS / 2);
         }
+    // tile u of this wave's in a step, and where its slot lies
+    auto tile_of = [&](int step, int u) { return (step * KW + kw) * TPS + u; };
+    auto keys_slot = [&](int step, int u) -> unsigned {
+        return (unsigned)((((unsigned)step % RING * KW + kw) * TPS + u) * 2 * TILEB);
+    };
+    auto values_slot = [&](int step, int u) -> unsigned { return keys_slot(step, u) + TILEB; };
     const int32_t *table = a.at.pages ? a.at.pages + (long long)pair * a.at.per_head : nullptr;
-    int page0 = 0, page1 = 0;                       // pages of the two halves of the tile that is fetched next
-    auto look_up = [&](int t) __attribute__((always_inline)) {
+    int page[2 * TPS];                              // of the halves of the tiles that are fetched next
+    auto look_up = [&](int step) __attribute__((always_inline)) {
         if (!table) return;
-        const int j0 = s_lo + 32 * min(t, n_tiles - 1);
-        page0 = uniform_word(table + (j0 >> a.at.shift));
-        page1 = uniform_word(table + min((j0 + 16) >> a.at.shift, a.at.per_head - 1));
-    };
-    unsigned bad = 0;                               // two bits per slot: this half of its tile lies in no page
-    auto fetch = [&](int step) __attribute__((always_inline)) {                    // this wave's part of step `step` (the last tile again past the end)
-        const int slot = step % RING, t = min(step * KW + kw, n_tiles - 1), j0 = s_lo + 32 * t;
-        const unsigned dst = lds0 + (unsigned)((slot * KW + kw) * 2 * TILEB);
-        long long r0 = (long long)pair * a.at.Lmax + j0, r1 = r0 + 16;      // rows of the halves
-        if (table) {
-            const int in = (1 << a.at.shift) - 1;
-            const bool no0 = (unsigned)page0 >= (unsigned)a.at.n_pages, no1 = (unsigned)page1 >= (unsigned)a.at.n_pages;
-            r0 = no0 ? 0 : ((long long)page0 << a.at.shift) + (j0 & in);
-            r1 = no1 ? 0 : ((long long)page1 << a.at.shift) + ((j0 + 16) & in);
-            bad = (bad & ~(3u << (2 * slot))) | ((no0 ? 1u : 0u) | (no1 ? 2u : 0u)) << (2 * slot);
-            look_up((step + 1) * KW + kw);
-        }
-        if (j0 + 32 <= s_hi) {
 #pragma unroll
-            for (int y = 0; y < NL; ++y) {
+        for (int u = 0; u < TPS; ++u) {
+            const int j0 = s_lo + 32 * min(tile_of(step, u), n_tiles - 1);
+            page[2 * u] = uniform_word(table + (j0 >> a.at.shift));
+            page[2 * u + 1] = uniform_word(table + min((j0 + 16) >> a.at.shift, a.at.per_head - 1));
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < 2 * TPS; ++i) page[i] = 0;
+    unsigned bad = 0;                               // two bits per tile of the ring: this half of it lies in no page
+    auto fetch = [&](int step) __attribute__((always_inline)) {     // this wave's part of a step (past the end the last tile again)
+        int at_page[2 * TPS];
+#pragma unroll
+        for (int i = 0; i < 2 * TPS; ++i) at_page[i] = page[i];
+        if (table) look_up(step + 1);
+#pragma unroll
+        for (int u = 0; u < TPS; ++u) {
+            const int t = min(tile_of(step, u), n_tiles - 1), j0 = s_lo + 32 * t;
+            long long r0 = (long long)pair * a.at.Lmax + j0, r1 = r0 + 16;      // rows of the halves
+            if (table) {
+                const int in = (1 << a.at.shift) - 1, p0 = at_page[2 * u], p1 = at_page[2 * u + 1];
+                const bool no0 = (unsigned)p0 >= (unsigned)a.at.n_pages, no1 = (unsigned)p1 >= (unsigned)a.at.n_pages;
+                const int at = 2 * ((unsigned)step % RING * TPS + u);
+                r0 = no0 ? 0 : ((long long)p0 << a.at.shift) + (j0 & in);
+                r1 = no1 ? 0 : ((long long)p1 << a.at.shift) + ((j0 + 16) & in);
+                bad = (bad & ~(3u << at)) | ((no0 ? 1u : 0u) | (no1 ? 2u : 0u)) << at;
+                if (no0 || no1) n_clear = min(n_clear, t);
+            }
+            // load y of the wave: x of the tile; the wave's loads lie in one half of one part (four waves), in one part (two), or
+            // anywhere
+            auto is_keys = [&](int y) { return RW == 1 ? y < LOADS / 2 : rw < RW / 2; };
+            auto is_lower = [&](int y) { return RW == 4 ? (rw & 1) == 0 : y % (LOADS / 2) < LOADS / 4; };
+            auto to = [&](int y) {
                 const int x = rw * NL + y;
-                const bool keys = x < LOADS / 2, lower = x % (LOADS / 2) < LOADS / 4;
-                const char *src = uniform_ptr((keys ? a.k : a.v) + (lower ? r0 : r1) * ROWB);
-                asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::
-                                 "v"(off[SETS == 2 ? y / (LOADS / 2) : 0][y % ND]), "s"(src), "s"(__builtin_amdgcn_readfirstlane(dst + 1024u * x))
-                             : "memory", "m0");
-            }
-        } else {                                    // rows past the last entry repeat it (and are masked)
-            const int last = s_hi - 1 - j0;
+                return __builtin_amdgcn_readfirstlane(lds0 + (is_keys(y) ? keys_slot(step, u) : values_slot(step, u)) + 1024u * (x % (LOADS / 2)));
+            };
+            if (j0 + 32 <= s_hi) {
+                const char *src = nullptr;
 #pragma unroll
-            for (int y = 0; y < NL; ++y) {
-                const int x = rw * NL + y, row = RPL * (x % (LOADS / 2)) + lane / UPR, from = min(row, last);
-                const bool keys = x < LOADS / 2;
-                const char *src = (keys ? a.k : a.v) + (((from & 16) ? r1 : r0) + (from & 15)) * ROWB + unit_of(row, keys);
-                asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src),
-                                 "s"(__builtin_amdgcn_readfirstlane(dst + 1024u * x))
-                             : "memory", "m0");
+                for (int y = 0; y < NL; ++y) {
+                    if (y % ND == 0) src = uniform_ptr((is_keys(y) ? a.k : a.v) + (is_lower(y) ? r0 : r1) * ROWB);
+                    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::
+                                     "v"(off[SETS == 2 ? y / (LOADS / 2) : 0][y % ND]), "s"(src), "s"(to(y))
+                                 : "memory", "m0");
+                }
+            } else {                                // rows past the last entry repeat it (and are masked)
+                int ln = lane;
+                asm volatile("" : "+v"(ln));        // (worked out here: kept from loop to loop, these addresses crowd the registers)
+                const int last = s_hi - 1 - j0;
+#pragma unroll
+                for (int y = 0; y < NL; ++y) {
+                    const int row = RPL * ((rw * NL + y) % (LOADS / 2)) + ln / UPR, from = min(row, last);
+                    const char *src = (is_keys(y) ? a.k : a.v) + (((from & 16) ? r1 : r0) + (from & 15)) * ROWB +
+                                      16 * ((ln % UPR) ^ (is_keys(y) ? place_k(row) : place_v(row)));
+                    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(to(y)) : "memory", "m0");
+                }
             }
         }
     };
-    if (n_steps > 0) look_up(kw);
-    for (int s = 0; s < min(RING - 1, n_steps); ++s) fetch(s);
-
     // ---- this wave's rows: lane holds row l32 of each block, half hf of the channels' contraction
     const int wrow0 = row0 + 32 * RB * rw;
-    uint4 qf[RB][NV];
+    typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+    u32x4 qf[RB][NV];
     int t_row[RB];
 #pragma unroll
     for (int x = 0; x < RB; ++x) {
@@ -186,27 +231,17 @@ __global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
         t_row[x] = row / a.G;
         const char *src = a.q + b * a.qsb + t_row[x] * a.qst + (long long)(g * a.G + row - t_row[x] * a.G) * a.qsh + 16 * hf;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) qf[x][i] = *reinterpret_cast<const uint4 *>(src + 32 * i);
+        for (int i = 0; i < NV; ++i) qf[x][i] = *reinterpret_cast<const u32x4 *>(src + 32 * i);
     }
     const bool idle = wrow0 >= n_live;              // (uniform) a wave without rows only helps to move the entries
 
     f32x16 o[RB][NCB];
-    float m[RB], l[RB];                             // l: of this lane's half
-#pragma unroll
-    for (int x = 0; x < RB; ++x) {
-        m[x] = -INFINITY;
-        l[x] = 0.f;
-#pragma unroll
-        for (int cb = 0; cb < NCB; ++cb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) o[x][cb][r] = 0.f;
-    }
+    float m[RB], l[RB];                             // m: log2 units; l: of this lane's half
     // LDS addresses within a tile
     unsigned ka[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) ka[i] = l32 * ROWB + 16 * ((2 * i + hf) ^ place_k(l32));
     // values: bf16, entries 4 hf + (l16 / 4) (+ 8 and 16 by immediates), channels 32 cb + 16 (lane / 16 % 2) + 4 (l16 % 4) ..
-    //         fp32, entry 4 hf (+ ...), channel 32 cb + l32
     unsigned va[NCB];
     {
         const int l16 = lane & 15, key = 4 * hf + (l16 >> 2), grp = (lane >> 4) & 1;
@@ -218,13 +253,19 @@ __global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
         return *reinterpret_cast<const float *>(vt + key * ROWB + 16 * ((8 * cb + (l32 >> 2)) ^ place_v(key)) + 4 * (l32 & 3));
     };
     typedef short v4i16 __attribute__((ext_vector_type(4)));
+    auto v_frag = [&](const char *vt, int cb, int h) {          // bf16: entries of accumulator registers 8 h .. 8 h + 7
+        const char *src = vt + va[cb] + 16 * h * ROWB;
+        const uint2 u0 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16 *)src));
+        const uint2 u1 = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                       (__attribute__((address_space(3))) v4i16 *)(src + 8 * ROWB)));
+        return make_uint4(u0.x, u0.y, u1.x, u1.y);
+    };
+    auto keys_at = [&](int step, int u) { return lds + keys_slot(step, u); };
+    auto values_at = [&](int step, int u) { return lds + values_slot(step, u); };
+    auto quad = [](const uint32_t (&p)[8], int h) { return make_uint4(p[4 * h], p[4 * h + 1], p[4 * h + 2], p[4 * h + 3]); };
 
-    // ---- one tile
-    auto tile = [&](int t, int slot, auto careful_tag) __attribute__((always_inline)) {
-        constexpr bool CAREFUL = decltype(careful_tag)::value;
-        const char *kt = lds + (slot * KW + kw) * 2 * TILEB, *vt = kt + TILEB;
-        const int j0 = s_lo + 32 * t;
-        f32x16 s[RB];
+    // logits of a tile
+    auto logits = [&](const char *kt, f32x16 (&s)[RB]) __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < RB; ++x)
 #pragma unroll
@@ -234,50 +275,110 @@ __global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
             const uint4 kf = *reinterpret_cast<const uint4 *>(kt + ka[i]);
 #pragma unroll
             for (int x = 0; x < RB; ++x) {
-                if constexpr (DT == LVLM_BF16) mfma_one<DT>(s[x], kf, qf[x][i], 0);
-                else
-#pragma unroll
-                    for (int c = 0; c < 4; ++c) mfma_one<DT>(s[x], kf, qf[x][i], c);
-            }
-        }
-        if constexpr (CAREFUL) {
-            // bit k: does this lane's row see entry j0 + k?
-            const int d = first - j0;               // entries before the drafts
-            unsigned in = s_hi - j0 >= 32 ? ~0u : s_hi > j0 ? (1u << (s_hi - j0)) - 1u : 0u;
-            if (bad >> (2 * slot) & 1u) in &= 0xffff0000u;
-            if (bad >> (2 * slot) & 2u) in &= 0x0000ffffu;
-#pragma unroll
-            for (int x = 0; x < RB; ++x) {
-                unsigned sees;
-                if (d >= 32) {
-                    sees = ~0u;
-                } else if (a.mask) {
-                    const uint32_t *w = a.mask + ((long long)b * a.T + t_row[x]) * a.words;
-                    if (d >= 0) {
-                        sees = (d ? (1u << d) - 1u : 0u) | w[0] << d;
-                    } else {
-                        const int at = (-d) >> 5, sh = (-d) & 31;
-                        const unsigned lo = at < a.words ? w[at] : 0u, hi = at + 1 < a.words ? w[at + 1] : 0u;
-                        sees = sh ? lo >> sh | hi << (32 - sh) : lo;
-                    }
+                if constexpr (DT == LVLM_BF16) {
+                    mfma_one<DT>(s[x], kf, __builtin_bit_cast(uint4, qf[x][i]), 0);
                 } else {
-                    const int upto = d + t_row[x];  // the last one seen
-                    sees = upto >= 31 ? ~0u : upto >= 0 ? (2u << upto) - 1u : 0u;
-                }
-                sees &= in;
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (!(sees >> acc_row(r, hf) & 1u)) s[x][r] = -INFINITY;
+                    for (int c = 0; c < 4; ++c) mfma_one<DT>(s[x], kf, __builtin_bit_cast(uint4, qf[x][i]), c);
+                }
             }
         }
-        // softmax: the reference follows the running maximum in steps
-        uint32_t pk[RB][8];
+    };
+    // a row's largest logit of the tile, in log2 units
+    auto largest = [&](const f32x16 &s) {
+        float mx = s[0];
+#pragma unroll
+        for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[r]);
+        return fmaxf(mx, other_half(mx)) * a.scale_log2;
+    };
+    // probabilities in place of the logits, relative to the reference; their sum
+    auto weigh = [&](f32x16 &s, float ref) {
+        float sum = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], a.scale_log2, -ref));
+            sum += s[r];
+        }
+        return sum;
+    };
+    auto add_values = [&](const char *vt, f32x16 (&s)[RB], bool odd) __attribute__((always_inline)) {
+        if constexpr (DT == LVLM_BF16) {
+            uint32_t pk[RB][8];
+#pragma unroll
+            for (int x = 0; x < RB; ++x)
+#pragma unroll
+                for (int r = 0; r < 8; ++r) pk[x][r] = pack_p(s[x][2 * r], s[x][2 * r + 1]);
+#pragma unroll
+            for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint4 vf = v_frag(vt, cb, h);
+                    if (odd) vf = make_uint4(Z::finite(vf.x), Z::finite(vf.y), Z::finite(vf.z), Z::finite(vf.w));
+#pragma unroll
+                    for (int x = 0; x < RB; ++x) mfma_one<DT>(o[x][cb], vf, quad(pk[x], h), 0);
+                }
+        } else {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+#pragma unroll
+                for (int cb = 0; cb < NCB; ++cb) {
+                    float v = v_float(vt, acc_row(r, 0) + 4 * hf, cb);
+                    if (odd) v = __uint_as_float(Z::finite(__float_as_uint(v)));
+#pragma unroll
+                    for (int x = 0; x < RB; ++x) o[x][cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[x][r], o[x][cb], 0, 0, 0);
+                }
+        }
+    };
+
+    // a tile that every row sees whole
+    auto clear_tile = [&](int step, bool first_one) __attribute__((always_inline)) {
+        const char *kt = keys_at(step, 0);
+        f32x16 s[RB];
+        logits(kt, s);
+        if (first_one)
+#pragma unroll
+            for (int x = 0; x < RB; ++x) m[x] = largest(s[x]);
+#pragma unroll
+        for (int x = 0; x < RB; ++x) l[x] += weigh(s[x], m[x]);
+        add_values(values_at(step, 0), s, false);
+    };
+
+    auto careful_tile = [&](int step, int u) __attribute__((always_inline)) {
+        const char *kt = keys_at(step, u), *vt = values_at(step, u);
+        const int j0 = s_lo + 32 * tile_of(step, u);
+        const unsigned nowhere = bad >> (2 * ((unsigned)step % RING * TPS + u)) & 3u;
+        const int d = first - j0;                   // entries before the drafts
+        // bit k of `sees`: does this lane's row see entry j0 + k?
+        unsigned in = s_hi - j0 >= 32 ? ~0u : (1u << (s_hi - j0)) - 1u, sees[RB];
+        if (nowhere & 1u) in &= 0xffff0000u;
+        if (nowhere & 2u) in &= 0x0000ffffu;
 #pragma unroll
         for (int x = 0; x < RB; ++x) {
-            float mx = s[x][0];
+            if (d >= 32) {
+                sees[x] = ~0u;
+            } else if (a.mask) {
+                const uint32_t *w = a.mask + ((long long)b * a.T + t_row[x]) * a.words;
+                if (d >= 0) {
+                    sees[x] = (d ? (1u << d) - 1u : 0u) | w[0] << d;
+                } else {
+                    const int at = (-d) >> 5, sh = (-d) & 31;
+                    const unsigned lo = at < a.words ? w[at] : 0u, hi = at + 1 < a.words ? w[at + 1] : 0u;
+                    sees[x] = sh ? lo >> sh | hi << (32 - sh) : lo;
+                }
+            } else {
+                const int upto = d + t_row[x];      // the last one seen
+                sees[x] = upto >= 31 ? ~0u : upto >= 0 ? (2u << upto) - 1u : 0u;
+            }
+            sees[x] &= in;
+        }
+        f32x16 s[RB];
+        logits(kt, s);
 #pragma unroll
-            for (int r = 1; r < 16; ++r) mx = fmaxf(mx, s[x][r]);
-            mx = fmaxf(mx, other_half(mx)) * a.scale_log2;
+        for (int x = 0; x < RB; ++x) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (!(sees[x] >> acc_row(r, hf) & 1u)) s[x][r] = -INFINITY;
+            const float mx = largest(s[x]);
             if (__builtin_amdgcn_ballot_w64(mx > m[x] + kLazyTree) != 0ull) {
                 const float to = fmaxf(m[x], mx), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[x] - to);
                 m[x] = to;
@@ -287,150 +388,255 @@ __global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
 #pragma unroll
                     for (int r = 0; r < 16; ++r) o[x][cb][r] *= f;
             }
-            const float ref = m[x] == -INFINITY ? 0.f : -m[x];
-            float sum = 0.f;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[x][r] = __builtin_amdgcn_exp2f(fmaf(s[x][r], a.scale_log2, ref));
-                sum += s[x][r];
-            }
-            l[x] += sum;
-            if constexpr (DT == LVLM_BF16) {
-                typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
-                typedef float f2 __attribute__((ext_vector_type(2)));
-#pragma unroll
-                for (int r = 0; r < 8; ++r)
-                    pk[x][r] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{s[x][2 * r], s[x][2 * r + 1]}, bf2));
-            }
+            l[x] += weigh(s[x], m[x] == -INFINITY ? 0.f : m[x]);
         }
-        // Values.  One that is no number must not reach the rows that do not see it -- their weight for it is 0, and 0 times it is
-        // not: in a tile that has any they are left out of the product, and added to the rows that do see them.
+        // A value that is no number must not reach the rows that do not see it -- their weight for it is 0, and 0 times it is
+        // not: in a tile that has any they are left out of the product, and added to the rows that do see them.  (One row, or
+        // none of the drafts in the tile: nothing is unseen but what repeats the last entry.)
         bool odd = false;
-        if constexpr (CAREFUL) {
-            for (int i = lane; i < TILEB / 16; i += 64) {
-                const uint4 u = *reinterpret_cast<const uint4 *>(vt + 16 * i);
-                odd |= Z::not_finite(u.x) | Z::not_finite(u.y) | Z::not_finite(u.z) | Z::not_finite(u.w);
+        if (nowhere || (d < 32 && n > 1)) {
+            uint32_t any = 0;
+#pragma unroll
+            for (int i = 0; i < TILEB / 1024; ++i) {
+                const uint4 u = *reinterpret_cast<const uint4 *>(vt + 16 * lane + 1024 * i);
+                any |= Z::not_finite(u.x) | Z::not_finite(u.y) | Z::not_finite(u.z) | Z::not_finite(u.w);
             }
-            odd = __builtin_amdgcn_ballot_w64(odd) != 0ull;
-            if (odd) {
+            odd = __builtin_amdgcn_ballot_w64(any != 0) != 0ull;
+        }
+        if (odd) {
+            uint16_t *p_s = reinterpret_cast<uint16_t *>(p_mem) + wave * (32 * Z::P_PITCH);
 #pragma unroll
-                for (int x = 0; x < RB; ++x) {
-                    wave_sync();
+            for (int x = 0; x < RB; ++x) {
+                wave_sync();
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) p_s[wave][acc_row(r, hf) * 33 + l32] = s[x][r];
-                    wave_sync();
-                    for (int key = 0; key < 32; ++key) {
-                        const float p = p_s[wave][key * 33 + l32];
-                        const char *row = vt + key * ROWB;
+                for (int r = 0; r < 16; ++r) p_s[acc_row(r, hf) * Z::P_PITCH + l32] = (uint16_t)pack_p(s[x][r], 0.f);
+                wave_sync();
+                for (int key = 0; key < 32; ++key) {
+                    const float p = bf16_to_f32(p_s[key * Z::P_PITCH + l32]);
+                    const char *row = vt + key * ROWB;
 #pragma unroll
-                        for (int cb = 0; cb < NCB; ++cb)
+                    for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
-                            for (int r4 = 0; r4 < 4; ++r4) {
-                                const int byte = (32 * cb + 8 * r4 + 4 * hf) * ES;
-                                const char *src = row + 16 * ((byte >> 4) ^ place_v(key)) + (byte & 15);
-                                uint32_t v[4];
-                                if constexpr (DT == LVLM_BF16) {
-                                    const uint2 u = *reinterpret_cast<const uint2 *>(src);
-                                    v[0] = u.x << 16; v[1] = u.x & 0xffff0000u;
-                                    v[2] = u.y << 16; v[3] = u.y & 0xffff0000u;
-                                } else {
-                                    const uint4 u = *reinterpret_cast<const uint4 *>(src);
-                                    v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
-                                }
-#pragma unroll
-                                for (int c = 0; c < 4; ++c)
-                                    if (!(p == 0.f) && (v[c] & 0x7f800000u) == 0x7f800000u)
-                                        o[x][cb][4 * r4 + c] = fmaf(p, __uint_as_float(v[c]), o[x][cb][4 * r4 + c]);
+                        for (int r4 = 0; r4 < 4; ++r4) {
+                            const int byte = (32 * cb + 8 * r4 + 4 * hf) * ES;
+                            const char *src = row + 16 * ((byte >> 4) ^ place_v(key)) + (byte & 15);
+                            uint32_t v[4];
+                            if constexpr (DT == LVLM_BF16) {
+                                const uint2 u = *reinterpret_cast<const uint2 *>(src);
+                                v[0] = u.x << 16; v[1] = u.x & 0xffff0000u;
+                                v[2] = u.y << 16; v[3] = u.y & 0xffff0000u;
+                            } else {
+                                const uint4 u = *reinterpret_cast<const uint4 *>(src);
+                                v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
                             }
-                    }
+#pragma unroll
+                            for (int c = 0; c < 4; ++c)
+                                if (!(p == 0.f) && (v[c] & 0x7f800000u) == 0x7f800000u)
+                                    o[x][cb][4 * r4 + c] = fmaf(p, __uint_as_float(v[c]), o[x][cb][4 * r4 + c]);
+                        }
                 }
             }
         }
-        if constexpr (DT == LVLM_BF16) {
-#pragma unroll
-            for (int cb = 0; cb < NCB; ++cb)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const char *src = vt + va[cb] + 16 * h * ROWB;
-                    const v4i16 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16 *)src);
-                    const v4i16 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) v4i16 *)(src + 8 * ROWB));
-                    const uint2 u0 = __builtin_bit_cast(uint2, lo), u1 = __builtin_bit_cast(uint2, hi);
-                    uint4 vf = make_uint4(u0.x, u0.y, u1.x, u1.y);
-                    if (CAREFUL && odd) vf = make_uint4(Z::finite(vf.x), Z::finite(vf.y), Z::finite(vf.z), Z::finite(vf.w));
-#pragma unroll
-                    for (int x = 0; x < RB; ++x)
-                        mfma_one<DT>(o[x][cb], vf, make_uint4(pk[x][4 * h], pk[x][4 * h + 1], pk[x][4 * h + 2], pk[x][4 * h + 3]), 0);
-                }
-        } else {
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-#pragma unroll
-                for (int cb = 0; cb < NCB; ++cb) {
-                    float v = v_float(vt, acc_row(r, 0) + 4 * hf, cb);
-                    if (CAREFUL && odd) v = __uint_as_float(Z::finite(__float_as_uint(v)));
-#pragma unroll
-                    for (int x = 0; x < RB; ++x) o[x][cb] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, s[x][r], o[x][cb], 0, 0, 0);
-                }
-        }
+        add_values(vt, s, odd);
     };
 
-    // step s: its tiles have landed, and the next one that fits the ring is under way
-    auto turn = [&](int s) __attribute__((always_inline)) {
-        const bool more = s + RING - 1 < n_steps;
+    // Step s is next: it has landed (piped: and the next step's keys), and the step at REACH is under way.  (Before step 0: only
+    // the latter.)  Careful, piped: the keys of step s are needed too, so theirs is not the place to fill yet.
+    int fetched = 0;                                // steps this wave has asked for
+    auto fetch_to = [&](int last) __attribute__((always_inline)) {
+        if (fetched <= last && fetched < n_steps) fetch(fetched++);
+    };
+    auto turn = [&](int s, bool careful) __attribute__((always_inline)) {
         if constexpr (RW == 1) {
             // the slot about to be filled was read for the step before: those reads have to be back
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            if (more) {
-                fetch(s + RING - 1);
-                asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NL * (RING - 1)) : "memory");
-            } else {
-                asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            }
+            fetch_to(s + Z::REACH);
+            if (s < 0) return;
+            if (s + Z::REACH < n_steps) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NL * TPS * Z::OPEN) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         } else {
-            // everybody's parts have landed, and everybody's reads of the step before are back
-            if (s + RING - 2 < n_steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NL * (RING - 2)) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-            if (more) fetch(s + RING - 1);
+            // everybody's parts have landed, and everybody's reads of the steps before are back
+            if (s >= 0) {
+                if (fetched < n_steps && !(Z::PIPED && careful)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NL * TPS * Z::OPEN) : "memory");
+                else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            }
+            if constexpr (Z::PIPED) fetch_to(s + Z::REACH - (rw >= RW / 2 ? 2 : careful ? 1 : 0));
+            else fetch_to(s + Z::REACH);
         }
     };
-    // tiles that every row sees whole, then the others (a loop each: no paths join around the accumulators)
-    int s = 0;
-    bool turned = false;
-    for (; s < n_steps; ++s) {
-        turn(s);
-        const int t = s * KW + kw;
-        if (s_lo + 32 * t + 32 > clear_to || (bad >> (2 * (s % RING)) & 3u)) {
-            turned = true;
-            break;
+
+    // The clear tiles from step 0 on, three at different stages at a time: while step s's logits become probabilities on the vector
+    // ALUs, the matrix pipe multiplies the next step's logits and adds the values of the step before.  It is cut into slots of one
+    // product and a share of the logits -- scaling, exponential and sum each a slot apart, so that no slot waits for its own results
+    // --, and a scheduling barrier behind each keeps the compiler from drawing the pieces apart again.  s: left at the first
+    // step that is not clear as a whole; returns whether its turn has been taken.
+    auto clear_run = [&](int &s) __attribute__((always_inline)) {
+        constexpr int NM = 2 * NV, NS = NM + 4 * NCB, LPS = 32 / NS;        // products of the logits; slots; logits to a slot
+        f32x16 sa[RB], sb[RB], zero;
+        uint32_t pa[RB][8], pb[RB][8];
+        uint4 kf[NV], vf[NV];
+        float neg[RB];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) zero[r] = 0.f;
+        logits(keys_at(0, 0), sa);
+#pragma unroll
+        for (int x = 0; x < RB; ++x) {
+            m[x] = largest(sa[x]);
+            neg[x] = -m[x];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) pa[x][i] = 0;
         }
-        if (!idle) tile(t, s % RING, std::false_type{});
-    }
-    for (; s < n_steps; ++s) {
-        if (!turned) turn(s);
-        turned = false;
-        const int t = s * KW + kw;
-        if (t < n_tiles && !idle) tile(t, s % RING, std::true_type{});
+        {
+            const char *kt = keys_at(0, 1);
+#pragma unroll
+            for (int i = 0; i < NV; ++i) kf[i] = *reinterpret_cast<const uint4 *>(kt + ka[i]);
+        }
+        auto mfma = [](const uint4 &x, const uint4 &y, const f32x16 &c) {
+            return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), c, 0, 0, 0);
+        };
+        // logits sin -> probabilities pout; the next logits into sout; probabilities pin of the step before into the sums
+        auto stage = [&](const char *vt, const char *kt, f32x16 (&sin)[RB], f32x16 (&sout)[RB], uint32_t (&pin)[RB][8], uint32_t (&pout)[RB][8])
+                        __attribute__((always_inline)) {
+#pragma unroll
+            for (int x = 0; x < RB; ++x)
+#pragma unroll
+                for (int cb = 0; cb < NCB; ++cb) asm volatile("" : "+a"(o[x][cb]));
+#pragma unroll
+            for (int x = 0; x < RB; ++x)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) asm volatile("" : "+a"(qf[x][i]));
+            asm volatile("" : "+a"(sin[0]), "+a"(sin[1]));
+            float e_arg[32], e_p[32], tile_sum[2];
+            auto stage_arg = [&](int el) { e_arg[el] = fmaf(sin[el >> 4][el & 15], a.scale_log2, neg[el >> 4]); };
+            auto stage_exp = [&](int el) { e_p[el] = __builtin_amdgcn_exp2f(e_arg[el]); };
+            auto stage_sum = [&](int el) {
+                const int x = el >> 4;
+                tile_sum[x] = (el & 15) ? tile_sum[x] + e_p[el] : e_p[el];
+                if ((el & 15) == 15) l[x] += tile_sum[x];
+                if (el & 1) pout[x][(el & 15) >> 1] = pack_p(e_p[el - 1], e_p[el]);
+            };
+#pragma unroll
+            for (int e = 0; e < LPS; ++e) stage_arg(e);
+#pragma unroll
+            for (int sl = 0; sl < NS; ++sl) {
+                const int x = sl & 1, c = (sl < NM ? sl : sl - NM) >> 1;    // block, step of the product
+                if (sl < NM) sout[x] = mfma(kf[c], __builtin_bit_cast(uint4, qf[x][c]), c == 0 ? zero : sout[x]);
+                else o[x][c >> 1] = mfma(vf[c], quad(pin[x], c & 1), o[x][c >> 1]);
+                __builtin_amdgcn_sched_barrier(0);
+                if (sl < NM && x == 0) vf[c] = v_frag(vt, c >> 1, c & 1);
+                if (sl >= NM && sl - NM < NV) kf[sl - NM] = *reinterpret_cast<const uint4 *>(kt + ka[sl - NM]);
+#pragma unroll
+                for (int e = LPS * sl; e < LPS * sl + LPS; ++e) {
+                    if (e + LPS < 32) stage_arg(e + LPS);
+                    stage_exp(e);
+                    if (e >= LPS) stage_sum(e - LPS);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int e = 32 - LPS; e < 32; ++e) stage_sum(e);
+            // (made here and not, as the compiler would have it, behind the branch where they are used)
+#pragma unroll
+            for (int x = 0; x < RB; ++x) {
+                asm volatile("" : "+v"(l[x]));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) asm volatile("" : "+v"(pout[x][i]));
+            }
+        };
+        bool taken = false;
+        for (;;) {
+            stage(values_at(s + RING - 1, 1), keys_at(s + 1, 0), sa, sb, pa, pb);
+            stage(values_at(s, 0), keys_at(s + 1, 1), sb, sa, pb, pa);
+            if (++s >= n_steps) break;
+            taken = tile_of(s, 1) >= n_clear;
+            turn(s, taken);
+            if (taken) break;
+        }
+        const char *vt = values_at(s + RING - 1, 1);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint4 f = v_frag(vt, i >> 1, i & 1);
+#pragma unroll
+            for (int x = 0; x < RB; ++x) o[x][i >> 1] = mfma(f, quad(pa[x], i & 1), o[x][i >> 1]);
+        }
+        return taken;
+    };
+
+    for (int pass = 0;; ++pass) {
+#pragma unroll
+        for (int x = 0; x < RB; ++x) {
+            m[x] = -INFINITY;
+            l[x] = 0.f;
+#pragma unroll
+            for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) o[x][cb][r] = 0.f;
+        }
+        fetched = 0;
+        if (n_steps > 0) look_up(0);
+        if (pass > 0) n_clear = 0;
+        // the clear tiles, then the others (a loop each: where paths join around the accumulators the compiler copies them)
+        int s = -Z::REACH;
+        bool turned = false;
+        if constexpr (Z::PIPED) {
+            // values of the step before the first: zero, as are their probabilities
+            char *none = lds + values_slot(RING - 1, TPS - 1);
+            for (int i = 64 * rw + lane; i < TILEB / 16; i += 64 * RW) *reinterpret_cast<uint4 *>(none + 16 * i) = make_uint4(0, 0, 0, 0);
+            for (; s < 0; ++s) turn(s, false);
+            if (n_steps > 0) {
+                const bool clear = tile_of(0, TPS - 1) < n_clear;
+                turn(0, !clear);
+                turned = clear && !idle ? clear_run(s) : true;
+            }
+        } else {
+            for (; s < n_steps; ++s) {
+                turn(s, false);
+                if (s < 0) continue;
+                if (tile_of(s, 0) >= n_clear) {
+                    turned = true;
+                    break;
+                }
+                if (!idle) clear_tile(s, s == 0);
+            }
+        }
+        for (; s < n_steps; ++s) {
+            __builtin_assume(s >= 0);
+            if (!turned) turn(s, true);
+            turned = false;
+#pragma unroll 1
+            for (int u = 0; u < TPS; ++u)
+                if (tile_of(s, u) < n_tiles && !idle) careful_tile(s, u);
+        }
+        // (a sum of NaN counts as a risk too)
+        bool risk = false;
+#pragma unroll
+        for (int x = 0; x < RB; ++x) risk |= !(l[x] < __builtin_amdgcn_exp2f(kRiskTree));
+        risk = __builtin_amdgcn_ballot_w64(risk) != 0ull && n_clear > 0 && !idle;
+        if (lane == 0) again_s[wave] = risk;
+        __syncthreads();                            // (and nobody reads tiles any more)
+        if (!(again_s[0] | again_s[1] | again_s[2] | again_s[3])) break;
+        __syncthreads();
     }
 
     // ---- the waves that shared the entries meet; rows leave whole
-#pragma unroll
-    for (int x = 0; x < RB; ++x) {
-        l[x] += other_half(l[x]);
-        if (hf == 0) {
-            m_s[wave][32 * x + l32] = m[x];
-            l_s[wave][32 * x + l32] = l[x];
-        }
-    }
-    __syncthreads();                                // (and nobody reads tiles any more)
     constexpr int P = Z::PITCH, TPR = HD / 4;       // threads per row: four channels each
 #pragma unroll
     for (int x = 0; x < RB; ++x) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < KW; ++w) top = fmaxf(top, m_s[w * RW + rw][32 * x + l32]);
-        const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[x] - top);
-        char *mine = lds + wave * (32 * P) + l32 * P;
         if (x > 0) __syncthreads();                 // the block before has been read
+        l[x] += other_half(l[x]);
+        if (hf == 0) {
+            m_s[wave][l32] = m[x];
+            l_s[wave][l32] = l[x];
+        }
+        float f = 1.f;
+        if constexpr (KW > 1) {
+            __syncthreads();
+            float top = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < KW; ++w) top = fmaxf(top, m_s[w * RW + rw][l32]);
+            f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[x] - top);
+        }
+        char *mine = lds + wave * (32 * P) + l32 * P;
 #pragma unroll
         for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
@@ -446,13 +652,13 @@ __global__ __launch_bounds__(256, 1) void tree_attn_kernel(TreeArgs a) {
             float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
             float tm = -INFINITY, tl = 0.f;
 #pragma unroll
-            for (int w = 0; w < KW; ++w) tm = fmaxf(tm, m_s[w * RW + rg][32 * x + rr]);
+            for (int w = 0; w < KW; ++w) tm = fmaxf(tm, m_s[w * RW + rg][rr]);
 #pragma unroll
             for (int w = 0; w < KW; ++w) {
                 const float4 y = *reinterpret_cast<const float4 *>(lds + (w * RW + rg) * (32 * P) + rr * P + 4 * c);
                 sum.x += y.x; sum.y += y.y; sum.z += y.z; sum.w += y.w;
-                const float mw = m_s[w * RW + rg][32 * x + rr];
-                tl += tm == -INFINITY ? 0.f : l_s[w * RW + rg][32 * x + rr] * __builtin_amdgcn_exp2f(mw - tm);
+                const float mw = m_s[w * RW + rg][rr];
+                tl += tm == -INFINITY ? 0.f : l_s[w * RW + rg][rr] * __builtin_amdgcn_exp2f(mw - tm);
             }
             if (a.n_split > 1) {
                 const long long at = ((long long)pair * a.n_split + split) * a.M + row;
@@ -524,9 +730,7 @@ TreeForm tree_form(const lvlm_tree_desc &d) {
         if (d.hd == 64) return M <= 32 ? TreeForm{1, 4} : TreeForm{2, 1};
         return M <= 64 ? TreeForm{1, 2} : TreeForm{1, 1};
     }
-    if (M <= 32) return {1, 4};
-    if (M <= 64) return {2, 4};
-    return M <= 128 ? TreeForm{2, 2} : TreeForm{2, 1};
+    return M <= 32 ? TreeForm{1, 4} : M <= 64 ? TreeForm{1, 2} : M <= 128 ? TreeForm{1, 1} : TreeForm{2, 1};
 }
 
 }  // namespace
@@ -536,7 +740,7 @@ TreeWs tree_ws(const lvlm_tree_desc &d) {
     const long long M = (long long)(d.Hq / d.Hkv) * d.T, pairs = (long long)d.B * d.Hkv;
     const int bound = d.len_bound > 0 ? d.len_bound : d.Lmax;
     const long long blocks = (M + f.rows() - 1) / f.rows();
-    const int step = 32 * f.kw;             // entries of a step
+    const int step = 32 * f.kw * (d.dtype == LVLM_BF16 && f.rb == 2 ? 2 : 1);      // entries of a step
     const long long steps = (bound + step - 1) / step;
     // enough workgroups for every compute unit, and runs of two steps at least
     long long split = std::max(1ll, std::min({512 / std::max(1ll, pairs * blocks), (steps + 1) / 2, 64ll}));
@@ -580,12 +784,12 @@ hipError_t launch_tree_attn(const Prof &prof, const lvlm_tree_desc &d, const Tre
         LVLM_LAUNCH(prof, (tree_attn_kernel<DT_, HD_, RB_, KW_>), grid, dim3(256), 0, prof.stream, a);
     prof.begin("tree_attn");
     LVLM_TREE(LVLM_BF16, 128, 1, 4)
-    LVLM_TREE(LVLM_BF16, 128, 2, 4)
-    LVLM_TREE(LVLM_BF16, 128, 2, 2)
+    LVLM_TREE(LVLM_BF16, 128, 1, 2)
+    LVLM_TREE(LVLM_BF16, 128, 1, 1)
     LVLM_TREE(LVLM_BF16, 128, 2, 1)
     LVLM_TREE(LVLM_BF16, 64, 1, 4)
-    LVLM_TREE(LVLM_BF16, 64, 2, 4)
-    LVLM_TREE(LVLM_BF16, 64, 2, 2)
+    LVLM_TREE(LVLM_BF16, 64, 1, 2)
+    LVLM_TREE(LVLM_BF16, 64, 1, 1)
     LVLM_TREE(LVLM_BF16, 64, 2, 1)
     LVLM_TREE(LVLM_F32, 128, 1, 2)
     LVLM_TREE(LVLM_F32, 128, 1, 1)
