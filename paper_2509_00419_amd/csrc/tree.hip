@@ -67,8 +67,8 @@ struct TreeShape {
     static constexpr int P_PITCH = 34, P_BYTES = 4 * 32 * P_PITCH * 2;
     static constexpr int RING_BYTES = RING * STEPB, MERGE_BYTES = 4 * 32 * PITCH;
     static constexpr int LDS = RING_BYTES + P_BYTES > MERGE_BYTES ? RING_BYTES + P_BYTES : MERGE_BYTES;
-    static_assert(RING >= 2 && LDS + 1040 <= (160 << 10) / PER_CU, "the next step's tiles travel while this one's are used");
-    static_assert(KW == 1 || !PIPED, "the waves of a piped workgroup take the same tiles, and load keys or values");
+    static_assert(RING >= 2 && LDS + 2064 <= (160 << 10) / PER_CU, "the next step's tiles travel while this one's are used");
+    static_assert(KW == 1 || RB == 1, "waves with two blocks of rows take the same tiles, and load keys or values");
     // a word of values (one, or two in bf16): is any of them NaN or infinite; the word with 0 in their place
     __device__ static __forceinline__ bool not_finite(uint32_t w) {
         return (w & 0x7f800000u) == 0x7f800000u || (DT == LVLM_BF16 && (w & 0x7f80u) == 0x7f80u);
@@ -105,6 +105,7 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
     __shared__ __attribute__((aligned(1024))) char lds[Z::LDS];
     __shared__ float m_s[4][32], l_s[4][32];
     __shared__ int again_s[4];
+    __shared__ long long at_s[4][32];               // where a row goes
     char *const p_mem = lds + Z::RING_BYTES;
 
     const int tid = threadIdx.x, lane = tid & 63;
@@ -121,11 +122,10 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
     const int split = __builtin_amdgcn_readfirstlane(unit / pairs), pair = __builtin_amdgcn_readfirstlane(unit % pairs);
     const int b = pair / a.Hkv, g = pair % a.Hkv;
     const int row0 = (seq % a.row_blocks) * Z::ROWS;
-    const int n = rows_in_use(a, b), n_live = n * a.G;
-    if (row0 >= n_live) return;
-    const int len = uniform_word(a.len + pair), L = min(max(len, 0), a.bound);
+    const int len = uniform_word(a.len + pair), n = rows_in_use(a, b), n_live = n * a.G;
+    const int L = min(max(len, 0), a.bound);
     const int s_lo = split * a.split_len, s_hi = min(L, s_lo + a.split_len);
-    if (s_lo >= s_hi && a.n_split > 1) return;
+    if (row0 >= n_live || (s_lo >= s_hi && a.n_split > 1)) return;
     const int first = max(len, 0) - n;              // entry of drafted row 0 (below 0: the head holds fewer than n)
     const int n_tiles = s_hi > s_lo ? (s_hi - s_lo + 31) >> 5 : 0;
     const int n_steps = (n_tiles + KW * TPS - 1) / (KW * TPS);
@@ -141,16 +141,16 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
     // Load x of a tile (keys first) fills bytes [1024 x, +1024): rows RPL x .. of its part, lane -> row lane / UPR, unit lane % UPR.
     // The rows of a half tile (16, in one page) are loaded from its first one on with these offsets.
     const unsigned lds0 = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char *)lds;
+    // Of load y of a half, the place of row RPL y + i differs from that of row i by the place of row RPL y: one offset, of the first
+    // load, gives all of them.
     constexpr int ND = 16 / RPL, SETS = RW == 1 ? 2 : 1;    // loads of a half; a wave loads keys and values, or one of them
-    unsigned off[SETS][ND];
-    auto unit_of = [&](int row, bool keys) { return 16 * ((lane % UPR) ^ (keys ? place_k(row) : place_v(row))); };
+    const bool loads_keys = rw < (RW + 1) / 2;              // (four waves, two: the first half of them)
+    unsigned off[SETS];
 #pragma unroll
-    for (int p = 0; p < SETS; ++p)
-#pragma unroll
-        for (int y = 0; y < ND; ++y) {
-            const int row = RPL * y + lane / UPR;
-            off[p][y] = row * ROWB + unit_of(row, SETS == 2 ? p == 0 : rw * NL < LOADS / 2);
-        }
+    for (int p = 0; p < SETS; ++p) {
+        const int row = lane / UPR;
+        off[p] = row * ROWB + 16 * ((lane % UPR) ^ ((SETS == 2 ? p == 0 : loads_keys) ? place_k(row) : place_v(row)));
+    }
     // tile u of this wave's in a step, and where its slot lies
     auto tile_of = [&](int step, int u) { return (step * KW + kw) * TPS + u; };
     auto keys_slot = [&](int step, int u) -> unsigned {
@@ -163,8 +163,8 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
         if (!table) return;
 #pragma unroll
         for (int u = 0; u < TPS; ++u) {
-            const int j0 = s_lo + 32 * min(tile_of(step, u), n_tiles - 1);
-            page[2 * u] = uniform_word(table + (j0 >> a.at.shift));
+            const int j0 = s_lo + 32 * tile_of(step, u);
+            page[2 * u] = uniform_word(table + min(j0 >> a.at.shift, a.at.per_head - 1));
             page[2 * u + 1] = uniform_word(table + min((j0 + 16) >> a.at.shift, a.at.per_head - 1));
         }
     };
@@ -187,24 +187,29 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
                 r0 = no0 ? 0 : ((long long)p0 << a.at.shift) + (j0 & in);
                 r1 = no1 ? 0 : ((long long)p1 << a.at.shift) + ((j0 + 16) & in);
                 bad = (bad & ~(3u << at)) | ((no0 ? 1u : 0u) | (no1 ? 2u : 0u)) << at;
-                if (no0 || no1) n_clear = min(n_clear, t);
+                if (no0 || no1) n_clear = min(n_clear, tile_of(step, u));
             }
-            // load y of the wave: x of the tile; the wave's loads lie in one half of one part (four waves), in one part (two), or
-            // anywhere
-            auto is_keys = [&](int y) { return RW == 1 ? y < LOADS / 2 : rw < RW / 2; };
-            auto is_lower = [&](int y) { return RW == 4 ? (rw & 1) == 0 : y % (LOADS / 2) < LOADS / 4; };
-            auto to = [&](int y) {
-                const int x = rw * NL + y;
-                return __builtin_amdgcn_readfirstlane(lds0 + (is_keys(y) ? keys_slot(step, u) : values_slot(step, u)) + 1024u * (x % (LOADS / 2)));
-            };
+            // the wave's loads, a half after the other: of one half of one part (four waves), of one part (two), or of all
             if (j0 + 32 <= s_hi) {
-                const char *src = nullptr;
 #pragma unroll
-                for (int y = 0; y < NL; ++y) {
-                    if (y % ND == 0) src = uniform_ptr((is_keys(y) ? a.k : a.v) + (is_lower(y) ? r0 : r1) * ROWB);
-                    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::
-                                     "v"(off[SETS == 2 ? y / (LOADS / 2) : 0][y % ND]), "s"(src), "s"(to(y))
-                                 : "memory", "m0");
+                for (int h = 0; h < NL / ND; ++h) {
+                    const bool keys = RW == 1 ? h < 2 : loads_keys, lower = RW == 4 ? (rw & 1) == 0 : (h & 1) == 0;
+                    const char *src = uniform_ptr((keys ? a.k : a.v) + (lower ? r0 : r1) * ROWB);
+                    const unsigned dst = lds0 + (keys ? keys_slot(step, u) : values_slot(step, u)) + (lower ? 0 : TILEB / 2);
+                    const unsigned o = off[RW == 1 ? h / 2 : 0];
+                    auto turned = [&](int y) { return o ^ (unsigned)(16 * (keys ? place_k(RPL * y) : place_v(RPL * y))); };
+                    // (the instruction's offset counts in memory and in LDS alike)
+                    if constexpr (ND == 2) {
+                        asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024"
+                                     ::"v"(o), "s"(src), "s"(__builtin_amdgcn_readfirstlane(dst)), "v"(turned(1)) : "memory", "m0");
+                    } else {
+#pragma unroll
+                        for (int y = 0; y < ND; y += 4)
+                            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
+                                         "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072"
+                                         ::"v"(turned(y)), "s"(src + 1024 * y), "s"(__builtin_amdgcn_readfirstlane(dst + 1024u * y)), "v"(turned(y + 1)),
+                                           "v"(turned(y + 2)), "v"(turned(y + 3)) : "memory", "m0");
+                    }
                 }
             } else {                                // rows past the last entry repeat it (and are masked)
                 int ln = lane;
@@ -212,10 +217,13 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
                 const int last = s_hi - 1 - j0;
 #pragma unroll
                 for (int y = 0; y < NL; ++y) {
-                    const int row = RPL * ((rw * NL + y) % (LOADS / 2)) + ln / UPR, from = min(row, last);
-                    const char *src = (is_keys(y) ? a.k : a.v) + (((from & 16) ? r1 : r0) + (from & 15)) * ROWB +
-                                      16 * ((ln % UPR) ^ (is_keys(y) ? place_k(row) : place_v(row)));
-                    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "s"(to(y)) : "memory", "m0");
+                    const int x = (rw * NL + y) % (LOADS / 2), row = RPL * x + ln / UPR, from = min(row, last);
+                    const bool keys = RW == 1 ? y < LOADS / 2 : loads_keys;
+                    const char *src = (keys ? a.k : a.v) + (((from & 16) ? r1 : r0) + (from & 15)) * ROWB +
+                                      16 * ((ln % UPR) ^ (keys ? place_k(row) : place_v(row)));
+                    const unsigned dst = lds0 + (keys ? keys_slot(step, u) : values_slot(step, u)) + 1024u * x;
+                    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src),
+                                     "s"(__builtin_amdgcn_readfirstlane(dst)) : "memory", "m0");
                 }
             }
         }
@@ -233,6 +241,14 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
 #pragma unroll
         for (int i = 0; i < NV; ++i) qf[x][i] = *reinterpret_cast<const u32x4 *>(src + 32 * i);
     }
+    uint32_t words[RB][2];                          // of the rows' masks, where two are all there are
+    if (a.mask && a.words <= 2)
+#pragma unroll
+        for (int x = 0; x < RB; ++x) {
+            const uint32_t *w = a.mask + ((long long)b * a.T + t_row[x]) * a.words;
+            words[x][0] = w[0];
+            words[x][1] = a.words > 1 ? w[1] : 0u;
+        }
     const bool idle = wrow0 >= n_live;              // (uniform) a wave without rows only helps to move the entries
 
     f32x16 o[RB][NCB];
@@ -343,7 +359,8 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
         add_values(values_at(step, 0), s, false);
     };
 
-    auto careful_tile = [&](int step, int u) __attribute__((always_inline)) {
+    auto careful_tile = [&](int step, int u, auto safe_tag) __attribute__((always_inline)) {
+        constexpr bool SAFE = decltype(safe_tag)::value;
         const char *kt = keys_at(step, u), *vt = values_at(step, u);
         const int j0 = s_lo + 32 * tile_of(step, u);
         const unsigned nowhere = bad >> (2 * ((unsigned)step % RING * TPS + u)) & 3u;
@@ -356,6 +373,9 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
         for (int x = 0; x < RB; ++x) {
             if (d >= 32) {
                 sees[x] = ~0u;
+            } else if (a.mask && a.words <= 2) {
+                const unsigned long long w = (unsigned long long)words[x][1] << 32 | words[x][0];
+                sees[x] = d >= 0 ? (d ? (1u << d) - 1u : 0u) | (unsigned)(w << d) : -d < 64 ? (unsigned)(w >> -d) : 0u;
             } else if (a.mask) {
                 const uint32_t *w = a.mask + ((long long)b * a.T + t_row[x]) * a.words;
                 if (d >= 0) {
@@ -379,14 +399,18 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
             for (int r = 0; r < 16; ++r)
                 if (!(sees[x] >> acc_row(r, hf) & 1u)) s[x][r] = -INFINITY;
             const float mx = largest(s[x]);
-            if (__builtin_amdgcn_ballot_w64(mx > m[x] + kLazyTree) != 0ull) {
-                const float to = fmaxf(m[x], mx), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[x] - to);
-                m[x] = to;
-                l[x] *= f;
+            if constexpr (SAFE) {
+                if (__builtin_amdgcn_ballot_w64(mx > m[x] + kLazyTree) != 0ull) {
+                    const float to = fmaxf(m[x], mx), f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[x] - to);
+                    m[x] = to;
+                    l[x] *= f;
 #pragma unroll
-                for (int cb = 0; cb < NCB; ++cb)
+                    for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
-                    for (int r = 0; r < 16; ++r) o[x][cb][r] *= f;
+                        for (int r = 0; r < 16; ++r) o[x][cb][r] *= f;
+                }
+            } else {
+                m[x] = m[x] == -INFINITY ? mx : m[x];       // (nothing has been added up yet)
             }
             l[x] += weigh(s[x], m[x] == -INFINITY ? 0.f : m[x]);
         }
@@ -395,13 +419,22 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
         // none of the drafts in the tile: nothing is unseen but what repeats the last entry.)
         bool odd = false;
         if (nowhere || (d < 32 && n > 1)) {
-            uint32_t any = 0;
+            // the largest exponent of all (in bf16 of both halves of a word)
+            typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+            u16x2 top2 = {0, 0};
+            uint32_t top = 0;
 #pragma unroll
             for (int i = 0; i < TILEB / 1024; ++i) {
-                const uint4 u = *reinterpret_cast<const uint4 *>(vt + 16 * lane + 1024 * i);
-                any |= Z::not_finite(u.x) | Z::not_finite(u.y) | Z::not_finite(u.z) | Z::not_finite(u.w);
+                const uint4 y = *reinterpret_cast<const uint4 *>(vt + 16 * lane + 1024 * i);
+                const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    if constexpr (DT == LVLM_BF16) top2 = __builtin_elementwise_max(top2, __builtin_bit_cast(u16x2, w[c] & 0x7fff7fffu));
+                    else top = max(top, w[c] & 0x7fffffffu);
+                }
             }
-            odd = __builtin_amdgcn_ballot_w64(any != 0) != 0ull;
+            odd = DT == LVLM_BF16 ? max(top2.x, top2.y) >= 0x7f80 : top >= 0x7f800000u;
+            odd = __builtin_amdgcn_ballot_w64(odd) != 0ull;
         }
         if (odd) {
             uint16_t *p_s = reinterpret_cast<uint16_t *>(p_mem) + wave * (32 * Z::P_PITCH);
@@ -562,7 +595,7 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
         return taken;
     };
 
-    for (int pass = 0;; ++pass) {
+    auto begin = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int x = 0; x < RB; ++x) {
             m[x] = -INFINITY;
@@ -574,8 +607,10 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
         }
         fetched = 0;
         if (n_steps > 0) look_up(0);
-        if (pass > 0) n_clear = 0;
-        // the clear tiles, then the others (a loop each: where paths join around the accumulators the compiler copies them)
+    };
+    begin();
+    // the clear tiles, then the others (a loop each: where paths join around the accumulators the compiler copies them)
+    {
         int s = -Z::REACH;
         bool turned = false;
         if constexpr (Z::PIPED) {
@@ -605,111 +640,166 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
             turned = false;
 #pragma unroll 1
             for (int u = 0; u < TPS; ++u)
-                if (tile_of(s, u) < n_tiles && !idle) careful_tile(s, u);
+                if (tile_of(s, u) < n_tiles && !idle) careful_tile(s, u, std::false_type{});
         }
-        // (a sum of NaN counts as a risk too)
+    }
+    // A row whose sum ran away from its reference (or is no number): the whole workgroup begins again, and rescales on the way.
+    {
         bool risk = false;
 #pragma unroll
         for (int x = 0; x < RB; ++x) risk |= !(l[x] < __builtin_amdgcn_exp2f(kRiskTree));
-        risk = __builtin_amdgcn_ballot_w64(risk) != 0ull && n_clear > 0 && !idle;
+        risk = __builtin_amdgcn_ballot_w64(risk) != 0ull && !idle;
         if (lane == 0) again_s[wave] = risk;
-        __syncthreads();                            // (and nobody reads tiles any more)
-        if (!(again_s[0] | again_s[1] | again_s[2] | again_s[3])) break;
+    }
+    __syncthreads();                                // (and nobody reads tiles any more)
+    if (again_s[0] | again_s[1] | again_s[2] | again_s[3]) {
+        begin();
+        for (int s = -Z::REACH; s < n_steps; ++s) {
+            turn(s, true);
+            if (s < 0) continue;
+#pragma unroll 1
+            for (int u = 0; u < TPS; ++u)
+                if (tile_of(s, u) < n_tiles && !idle) careful_tile(s, u, std::true_type{});
+        }
         __syncthreads();
     }
 
-    // ---- the waves that shared the entries meet; rows leave whole
-    constexpr int P = Z::PITCH, TPR = HD / 4;       // threads per row: four channels each
+    // ---- the waves that shared the entries meet, and rows leave whole: a lane scales its row's sums for good (it knows what the
+    // other waves have of the row), and what eight channels to a lane add up from LDS goes out as it is
+    constexpr int P = Z::PITCH, TPR = HD / 8;       // threads per row
 #pragma unroll
     for (int x = 0; x < RB; ++x) {
-        if (x > 0) __syncthreads();                 // the block before has been read
+        const int row = wrow0 + 32 * x + l32;
+        const bool shown = row < n_live;
         l[x] += other_half(l[x]);
-        if (hf == 0) {
-            m_s[wave][l32] = m[x];
-            l_s[wave][l32] = l[x];
-        }
-        float f = 1.f;
+        float top = m[x], sum = l[x], f = 1.f;
         if constexpr (KW > 1) {
+            if (hf == 0) {
+                m_s[wave][l32] = m[x];
+                l_s[wave][l32] = l[x];
+            }
             __syncthreads();
-            float top = -INFINITY;
 #pragma unroll
             for (int w = 0; w < KW; ++w) top = fmaxf(top, m_s[w * RW + rw][l32]);
-            f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[x] - top);
+            const float ref = top == -INFINITY ? 0.f : top;
+            f = __builtin_amdgcn_exp2f(m[x] - ref);
+            sum = 0.f;
+#pragma unroll
+            for (int w = 0; w < KW; ++w) sum = fmaf(l_s[w * RW + rw][l32], __builtin_amdgcn_exp2f(m_s[w * RW + rw][l32] - ref), sum);
         }
-        char *mine = lds + wave * (32 * P) + l32 * P;
+        const int head = g * a.G + row - t_row[x] * a.G;
+        const long long at = ((long long)pair * a.n_split + split) * a.M + row;
+        if (a.n_split == 1) f = sum == 0.f ? 0.f : f / sum;
+        if (kw == 0 && hf == 0 && shown) {
+            if (a.n_split > 1) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(top, sum);
+            else if (a.row_lse) a.row_lse[((long long)b * a.Hq + head) * a.T + t_row[x]] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * (1.f / kLog2e);
+        }
+        if (kw == 0 && hf == 0) at_s[rw][l32] = a.n_split > 1 ? at * (HD * 4) : b * a.osb + t_row[x] * a.ost + head * a.osh;
+        if (shown) {
+            char *mine = lds + wave * (32 * P) + l32 * P;
 #pragma unroll
-        for (int cb = 0; cb < NCB; ++cb)
+            for (int cb = 0; cb < NCB; ++cb)
 #pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4)
-                *reinterpret_cast<float4 *>(mine + (32 * cb + 8 * r4 + 4 * hf) * 4) =
-                    make_float4(o[x][cb][4 * r4] * f, o[x][cb][4 * r4 + 1] * f, o[x][cb][4 * r4 + 2] * f, o[x][cb][4 * r4 + 3] * f);
-        __syncthreads();
-        // rows of this pass: RW groups of 32
-        for (int i = tid; i < 32 * RW * TPR; i += 256) {
-            const int r = i / TPR, c = 4 * (i % TPR), rg = r >> 5, rr = r & 31;
-            const int row = row0 + 32 * (RB * rg + x) + rr;
-            if (row >= n_live) continue;
-            float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-            float tm = -INFINITY, tl = 0.f;
+                for (int r4 = 0; r4 < 4; ++r4)
+                    *reinterpret_cast<float4 *>(mine + (32 * cb + 8 * r4 + 4 * hf) * 4) =
+                        make_float4(o[x][cb][4 * r4] * f, o[x][cb][4 * r4 + 1] * f, o[x][cb][4 * r4 + 2] * f, o[x][cb][4 * r4 + 3] * f);
+        }
+        if constexpr (KW > 1) __syncthreads();
+        else wave_sync();
+        // KW = 1: each wave its own rows; else all threads the workgroup's
+        constexpr int STRIDE = (KW > 1 ? 256 : 64) / TPR, COUNT = (KW > 1 ? 32 * RW : 32) / STRIDE;
+        const int i0 = (KW > 1 ? tid : lane) / TPR, c = 8 * (lane % TPR);
+        const char *base = a.n_split > 1 ? reinterpret_cast<const char *>(a.part_o) : a.out;
 #pragma unroll
-            for (int w = 0; w < KW; ++w) tm = fmaxf(tm, m_s[w * RW + rg][rr]);
+        for (int i = 0; i < COUNT; ++i) {
+            const int r = i0 + STRIDE * i, rg = KW > 1 ? r >> 5 : rw, rr = r & 31;
+            if (row0 + 32 * (RB * rg + x) + rr >= n_live) continue;
+            float4 y0 = make_float4(0.f, 0.f, 0.f, 0.f), y1 = y0;
 #pragma unroll
             for (int w = 0; w < KW; ++w) {
-                const float4 y = *reinterpret_cast<const float4 *>(lds + (w * RW + rg) * (32 * P) + rr * P + 4 * c);
-                sum.x += y.x; sum.y += y.y; sum.z += y.z; sum.w += y.w;
-                const float mw = m_s[w * RW + rg][rr];
-                tl += tm == -INFINITY ? 0.f : l_s[w * RW + rg][rr] * __builtin_amdgcn_exp2f(mw - tm);
+                const float4 *src = reinterpret_cast<const float4 *>(lds + (w * RW + rg) * (32 * P) + rr * P + 4 * c);
+                const float4 z0 = src[0], z1 = src[1];
+                y0 = w ? make_float4(y0.x + z0.x, y0.y + z0.y, y0.z + z0.z, y0.w + z0.w) : z0;
+                y1 = w ? make_float4(y1.x + z1.x, y1.y + z1.y, y1.z + z1.z, y1.w + z1.w) : z1;
             }
-            if (a.n_split > 1) {
-                const long long at = ((long long)pair * a.n_split + split) * a.M + row;
-                *reinterpret_cast<float4 *>(a.part_o + at * HD + c) = sum;
-                if (c == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(tm, tl);
+            char *dst = const_cast<char *>(base) + at_s[rg][rr];
+            if (DT == LVLM_F32 || a.n_split > 1) {
+                reinterpret_cast<float4 *>(dst + 4 * c)[0] = y0;
+                reinterpret_cast<float4 *>(dst + 4 * c)[1] = y1;
             } else {
-                const int t = row / a.G, h = g * a.G + row - t * a.G;
-                const float inv = tl == 0.f ? 0.f : 1.f / tl;
-                char *dst = a.out + b * a.osb + t * a.ost + h * a.osh + c * ES;
-                if (tl == 0.f) sum = make_float4(0.f, 0.f, 0.f, 0.f);
-                if constexpr (DT == LVLM_BF16) {
-                    *reinterpret_cast<ushort4 *>(dst) = make_ushort4(f32_to_bf16(sum.x * inv), f32_to_bf16(sum.y * inv),
-                                                                     f32_to_bf16(sum.z * inv), f32_to_bf16(sum.w * inv));
-                } else {
-                    *reinterpret_cast<float4 *>(dst) = make_float4(sum.x * inv, sum.y * inv, sum.z * inv, sum.w * inv);
-                }
-                if (c == 0 && a.row_lse)
-                    a.row_lse[((long long)b * a.Hq + h) * a.T + t] = tl == 0.f ? -INFINITY : (tm + __builtin_amdgcn_logf(tl)) * (1.f / kLog2e);
+                *reinterpret_cast<uint4 *>(dst + 2 * c) = make_uint4(pack_p(y0.x, y0.y), pack_p(y0.z, y0.w), pack_p(y1.x, y1.y), pack_p(y1.z, y1.w));
             }
         }
+        if constexpr (RB > 1) wave_sync();          // (only waves of their own rows have a second block)
     }
 }
 
-// Folds the runs of a pair's entries: four channels of a row to a thread.
+// Folds the runs of a pair's entries: a row to HD / 4 threads, four channels each.  Lane i of them looks at run i (and further ones):
+// the maxima and sums of all runs come in one round trip, the sums of p v eight runs at a time.
 template <int DT, int HD>
 __global__ __launch_bounds__(256) void tree_fold_kernel(TreeArgs a) {
-    constexpr int ES = esize<DT>(), TPR = HD / 4;
+    constexpr int ES = esize<DT>(), TPR = HD / 4, PER = 64 / TPR, AT_ONCE = 8;      // threads per row; runs per lane
     const int pair = blockIdx.y, b = pair / a.Hkv, g = pair % a.Hkv;
-    const int row = blockIdx.x * (256 / TPR) + threadIdx.x / TPR, c = 4 * (threadIdx.x % TPR);
-    const int n_live = rows_in_use(a, b) * a.G;
-    if (row >= n_live) return;
-    const int L = min(max(uniform_word(a.len + pair), 0), a.bound), used = (L + a.split_len - 1) / a.split_len;
-    const long long at = (long long)pair * a.n_split * a.M + row;
-    float top = -INFINITY;
-    for (int s = 0; s < used; ++s) top = fmaxf(top, a.part_ml[(at + (long long)s * a.M) * 2]);
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    const int li = threadIdx.x % TPR, c = 4 * li, row = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
+    const int n_live = rows_in_use(a, b) * a.G, L = min(max(uniform_word(a.len + pair), 0), a.bound);
+    if ((int)blockIdx.x * (256 / TPR) >= n_live) return;
+    const int used = (L + a.split_len - 1) / a.split_len;
+    const bool live = row < n_live;
+    const long long at = (long long)pair * a.n_split * a.M + min(row, n_live - 1);
+    float m[PER], w[PER], top = -INFINITY;
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+        const int s = li + TPR * x;
+        const float2 ml = s < used ? *reinterpret_cast<const float2 *>(a.part_ml + (at + (long long)s * a.M) * 2) : make_float2(-INFINITY, 0.f);
+        m[x] = ml.x;
+        w[x] = ml.y;
+        top = fmaxf(top, ml.x);
+    }
+    auto over_row = [](float v, auto op) {          // over the TPR lanes of the row
+        v = op(v, dpp_quad1(v));
+        v = op(v, dpp_quad2(v));
+        v = op(v, dpp_half_mirror(v));
+        v = op(v, dpp_row_mirror(v));
+        return TPR == 32 ? op(v, swap_rows(v)) : v;
+    };
+    top = over_row(top, [](float x, float y) { return fmaxf(x, y); });
     float l = 0.f;
-    if (top != -INFINITY)
-        for (int s = 0; s < used; ++s) {
-            const float2 ml = *reinterpret_cast<const float2 *>(a.part_ml + (at + (long long)s * a.M) * 2);
-            const float4 y = *reinterpret_cast<const float4 *>(a.part_o + (at + (long long)s * a.M) * HD + c);
-            const float f = __builtin_amdgcn_exp2f(ml.x - top);
-            l += ml.y * f;
-            sum.x = fmaf(y.x, f, sum.x);
-            sum.y = fmaf(y.y, f, sum.y);
-            sum.z = fmaf(y.z, f, sum.z);
-            sum.w = fmaf(y.w, f, sum.w);
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+        const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[x] - top);
+        l += w[x] * f;
+        w[x] = f;                                   // from here on the run's weight
+    }
+    l = over_row(l, [](float x, float y) { return x + y; });
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    const float *po = a.part_o + at * HD + c;
+    const int lane0 = (threadIdx.x & 63) - li;
+    for (int s0 = 0; s0 < used; s0 += AT_ONCE) {
+        float4 y[AT_ONCE];
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i)
+            y[i] = *reinterpret_cast<const float4 *>(po + (long long)min(s0 + i, used - 1) * a.M * HD);
+#pragma unroll
+        for (int i = 0; i < AT_ONCE; ++i) {
+            const int s = min(s0 + i, used - 1);
+            float f = 0.f;
+#pragma unroll
+            for (int x = 0; x < PER; ++x) {
+                const float g = __shfl(w[x], lane0 + s % TPR);
+                if (s / TPR == x) f = g;
+            }
+            if (s0 + i >= used) f = 0.f;
+            sum.x = fmaf(y[i].x, f, sum.x);
+            sum.y = fmaf(y[i].y, f, sum.y);
+            sum.z = fmaf(y[i].z, f, sum.z);
+            sum.w = fmaf(y[i].w, f, sum.w);
         }
+    }
+    if (!live) return;
     const int t = row / a.G, h = g * a.G + row - t * a.G;
     const float inv = l == 0.f ? 0.f : 1.f / l;
     char *dst = a.out + b * a.osb + t * a.ost + h * a.osh + c * ES;
+    if (l == 0.f) sum = make_float4(0.f, 0.f, 0.f, 0.f);
     if constexpr (DT == LVLM_BF16) {
         *reinterpret_cast<ushort4 *>(dst) =
             make_ushort4(f32_to_bf16(sum.x * inv), f32_to_bf16(sum.y * inv), f32_to_bf16(sum.z * inv), f32_to_bf16(sum.w * inv));
