@@ -161,6 +161,7 @@ AttnWs attn_ws(const lvlm_attn_desc &d);
 
 struct TreeWs {
     size_t part_o, part_ml, total;
+    int form;                   // which kernel: rows of a workgroup
     int n_split, split_len;     // runs of a pair's entries (split_len each), folded by a second launch
     int row_blocks;             // workgroups a pair's rows take
 };

@@ -24,7 +24,7 @@ struct TreeArgs {
     float *part_ml;     // [pair][split][row][2]   that maximum (logits times scale, base 2) and the sum of p
     CachePlace at;
     int B, T, Hq, Hkv, G, words, bound, M;      // M: T * G rows to a pair
-    int n_split, split_len, row_blocks;
+    int n_split, split_len, row_blocks, per_xcd;
     float scale_log2;
     long long qsb, qst, qsh, osb, ost, osh;     // bytes
 };
@@ -114,14 +114,15 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
     const int hf = lane >> 5, l32 = lane & 31;
 
     // Numbers with the same remainder modulo 8 run on one XCD: the row blocks of a run of entries follow each other there and
-    // share its L2; runs of different pairs alternate, so that a pair's empty runs fall on all XCDs alike.
-    const int pairs = a.B * a.Hkv;
-    const int seq = (int)(blockIdx.x >> 3);
-    const int unit = seq / a.row_blocks * 8 + (int)(blockIdx.x & 7);
-    if (unit >= pairs * a.n_split) return;
+    // share its L2.  Runs of different pairs alternate over the XCDs, so that a pair's empty runs fall on all of them alike; too few
+    // runs for that are dealt out evenly, row block by row block (4 pairs of 48 row blocks: 11.3 -> 7.6 us).
+    const int pairs = a.B * a.Hkv, xcd = blockIdx.x & 7, seq = (int)(blockIdx.x >> 3);
+    const int item = a.per_xcd ? xcd * a.per_xcd + seq : (seq / a.row_blocks * 8 + xcd) * a.row_blocks + seq % a.row_blocks;
+    const int unit = item / a.row_blocks;
+    if (unit >= pairs * a.n_split || (a.per_xcd && seq >= a.per_xcd)) return;
     const int split = __builtin_amdgcn_readfirstlane(unit / pairs), pair = __builtin_amdgcn_readfirstlane(unit % pairs);
     const int b = pair / a.Hkv, g = pair % a.Hkv;
-    const int row0 = (seq % a.row_blocks) * Z::ROWS;
+    const int row0 = (item % a.row_blocks) * Z::ROWS;
     const int len = uniform_word(a.len + pair), n = rows_in_use(a, b), n_live = n * a.G;
     const int L = min(max(len, 0), a.bound);
     const int s_lo = split * a.split_len, s_hi = min(L, s_lo + a.split_len);
@@ -190,7 +191,7 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
                 if (no0 || no1) n_clear = min(n_clear, tile_of(step, u));
             }
             // the wave's loads, a half after the other: of one half of one part (four waves), of one part (two), or of all
-            if (j0 + 32 <= s_hi) {
+            if (__builtin_expect(j0 + 32 <= s_hi, true)) {
 #pragma unroll
                 for (int h = 0; h < NL / ND; ++h) {
                     const bool keys = RW == 1 ? h < 2 : loads_keys, lower = RW == 4 ? (rw & 1) == 0 : (h & 1) == 0;
@@ -436,7 +437,7 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
             odd = DT == LVLM_BF16 ? max(top2.x, top2.y) >= 0x7f80 : top >= 0x7f800000u;
             odd = __builtin_amdgcn_ballot_w64(odd) != 0ull;
         }
-        if (odd) {
+        if (__builtin_expect(odd, false)) {         // (said, so that registers go to the common case)
             uint16_t *p_s = reinterpret_cast<uint16_t *>(p_mem) + wave * (32 * Z::P_PITCH);
 #pragma unroll
             for (int x = 0; x < RB; ++x) {
@@ -652,7 +653,7 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
         if (lane == 0) again_s[wave] = risk;
     }
     __syncthreads();                                // (and nobody reads tiles any more)
-    if (again_s[0] | again_s[1] | again_s[2] | again_s[3]) {
+    if (__builtin_expect(again_s[0] | again_s[1] | again_s[2] | again_s[3], 0)) {
         begin();
         for (int s = -Z::REACH; s < n_steps; ++s) {
             turn(s, true);
@@ -809,41 +810,75 @@ __global__ __launch_bounds__(256) void tree_fold_kernel(TreeArgs a) {
     if (c == 0 && a.row_lse) a.row_lse[((long long)b * a.Hq + h) * a.T + t] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * (1.f / kLog2e);
 }
 
-// Rows of a workgroup and how its waves share entries and rows.
+// How a call is cut: rows of a workgroup (32, 64, 128 or 256, by how its waves share entries and rows), and runs of a pair's
+// entries.  Many rows to a workgroup read an entry for all of them at once; few rows make many workgroups of few tiles each; runs
+// make more still, and cost a second launch that folds their sums.  What a cut takes is put together from the numbers below, and
+// the cut that takes least is done.  The numbers are a fit to the times of 766 shapes (4 to 512 pairs, 1 to 1536 rows, 64 to
+// 16384 entries, both types and head dimensions) in all forms and up to 64 runs; the cut they choose takes 0.6 % longer than the
+// shape's best on average, 26 % at most.  Against splitting until there are 512 workgroups and 256 rows where there are more than
+// 128, us: 4 pairs x 28 rows x 512 entries of 128 channels 12.6 -> 7.8, 8 x 384 x 2048 35 -> 17, 32 x 384 x 512 32 -> 13, 64 x 1 x
+// 2048 23 -> 16, 128 x 192 x 2048 72 -> 44, 512 x 768 x 128 117 -> 70; with 256 rows where they are right 32 x 384 x 16384
+// 160 -> 134.
 struct TreeForm {
-    int rb, kw;
+    int rb, kw, tps;        // blocks of 32 rows to a wave; waves side by side over entries; tiles of a wave in a step
+    float workgroup, tile;  // us: a workgroup without entries; a tile of 32 entries in one of its waves
+    float shared;           // workgroups that share a compute unit, of what they would take in turn (1: they do not share)
+    float alone;            // bytes per us that a workgroup gets from memory (1.6 times as many where the cache holds all entries)
+    float busy;             // us of a compute unit for a tile of one row block, on a chip that has all it can do
     int rows() const { return 32 * rb * (4 / kw); }
 };
-TreeForm tree_form(const lvlm_tree_desc &d) {
-    const int M = d.Hq / d.Hkv * d.T;
-    if (d.dtype == LVLM_F32) {
-        if (d.hd == 64) return M <= 32 ? TreeForm{1, 4} : TreeForm{2, 1};
-        return M <= 64 ? TreeForm{1, 2} : TreeForm{1, 1};
-    }
-    return M <= 32 ? TreeForm{1, 4} : M <= 64 ? TreeForm{1, 2} : M <= 128 ? TreeForm{1, 1} : TreeForm{2, 1};
+constexpr int kTreeForms = 4;
+const TreeForm *tree_forms(const lvlm_tree_desc &d, int &n) {
+    static constexpr TreeForm kBf16[2][kTreeForms] = {
+        {{1, 4, 1, 3.6f, 0.69f, 0.66f, 180e3f, 0.07f}, {1, 2, 1, 3.6f, 0.75f, 0.63f, 52e3f, 0.29f},
+         {1, 1, 1, 3.7f, 0.69f, 0.62f, 8.5e3f, 0.11f}, {2, 1, 2, 8.9f, 0.58f, 1.f, 92e3f, 0.74f}},
+        {{1, 4, 1, 4.2f, 0.77f, 1.f, 53e3f, 0.14f}, {1, 2, 1, 3.9f, 0.69f, 0.81f, 20e3f, 0.39f},
+         {1, 1, 1, 4.5f, 0.82f, 0.62f, 14.5e3f, 0.68f}, {2, 1, 2, 8.6f, 0.92f, 1.f, 92e3f, 0.71f}}};
+    static constexpr TreeForm kF32[2][3] = {
+        {{1, 4, 1, 4.1f, 2.8f, 1.f, 34e3f, 0.78f}, {1, 2, 1, 4.3f, 2.5f, 1.f, 14e3f, 1.5f}, {1, 1, 1, 4.4f, 2.4f, 1.f, 29e3f, 2.8f}},
+        {{1, 2, 1, 5.7f, 5.0f, 1.f, 52e3f, 2.8f}, {1, 1, 1, 6.9f, 4.4f, 1.f, 56e3f, 5.3f}, {}}};
+    n = d.dtype == LVLM_BF16 ? kTreeForms : d.hd == 64 ? 3 : 2;
+    return d.dtype == LVLM_BF16 ? kBf16[d.hd == 128] : kF32[d.hd == 128];
 }
 
 }  // namespace
 
 TreeWs tree_ws(const lvlm_tree_desc &d) {
-    const TreeForm f = tree_form(d);
+    constexpr int kUnits = 256;             // compute units
     const long long M = (long long)(d.Hq / d.Hkv) * d.T, pairs = (long long)d.B * d.Hkv;
-    const int bound = d.len_bound > 0 ? d.len_bound : d.Lmax;
-    const long long blocks = (M + f.rows() - 1) / f.rows();
-    const int step = 32 * f.kw * (d.dtype == LVLM_BF16 && f.rb == 2 ? 2 : 1);      // entries of a step
-    const long long steps = (bound + step - 1) / step;
-    // enough workgroups for every compute unit, and runs of two steps at least
-    long long split = std::max(1ll, std::min({512 / std::max(1ll, pairs * blocks), (steps + 1) / 2, 64ll}));
-    const long long run = (steps + split - 1) / split;
-    split = (steps + run - 1) / run;
-    TreeWs w;
-    w.n_split = (int)split;
-    w.split_len = (int)(run * step);
-    w.row_blocks = (int)blocks;
-    w.part_o = w.part_ml = w.total = 0;
-    if (split > 1) {
-        w.part_ml = align_up((size_t)(pairs * split * M) * d.hd * 4, 256);
-        w.total = w.part_ml + align_up((size_t)(pairs * split * M) * 8, 256);
+    const int bound = d.len_bound > 0 ? d.len_bound : d.Lmax, es = d.dtype == LVLM_BF16 ? 2 : 4;
+    const double bytes = (double)pairs * bound * d.hd * es * 2, tiles = (double)pairs * bound / 32 / kUnits;
+    int n_forms;
+    const TreeForm *forms = tree_forms(d, n_forms);
+    TreeWs w{};
+    double best = 0;
+    for (int i = 0; i < n_forms; ++i) {
+        const TreeForm &f = forms[i];
+        const int step = 32 * f.kw * f.tps;
+        const long long blocks = (M + f.rows() - 1) / f.rows(), steps = ((long long)bound + step - 1) / step;
+        for (int wanted : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+            if (wanted > steps) break;
+            const long long run = (steps + wanted - 1) / wanted, split = (steps + run - 1) / run;
+            if (pairs * blocks * split >= (1ll << 27)) break;
+            const double per_unit = (double)(pairs * blocks * split) / kUnits, whole = (double)((pairs * blocks * split + kUnits - 1) / kUnits);
+            const double rounds = per_unit > 8 ? per_unit : whole;
+            double t = (f.workgroup + f.tile * (double)(run * f.tps)) * (rounds <= 1 ? 1.0 : rounds * f.shared);
+            t = std::max(t, f.workgroup + (double)std::min<long long>(run * step, bound) * d.hd * es * 2 / (f.alone * (bytes > 200e6 ? 1.0 : 1.6)));
+            t = std::max(t, f.workgroup + std::max(bytes / 14e6, tiles * f.busy) * (double)blocks);      // 14 TB/s from the L2s
+            t = std::max(t, 1.0 + bytes / 7e6);                                                          // ... 7 from memory
+            if (split > 1) t += 6.0 + (double)pairs * split * M * d.hd * 8 / 5.5e6;
+            if (w.n_split == 0 || t < best) {
+                best = t;
+                w.form = i;
+                w.n_split = (int)split;
+                w.split_len = (int)(run * step);
+                w.row_blocks = (int)blocks;
+            }
+        }
+    }
+    if (w.n_split > 1) {
+        w.part_ml = align_up((size_t)(pairs * w.n_split * M) * d.hd * 4, 256);
+        w.total = w.part_ml + align_up((size_t)(pairs * w.n_split * M) * 8, 256);
     }
     return w;
 }
@@ -866,9 +901,11 @@ hipError_t launch_tree_attn(const Prof &prof, const lvlm_tree_desc &d, const Tre
     a.scale_log2 = d.scale * kLog2e;
     a.qsb = d.q_stride_b * es; a.qst = d.q_stride_t * es; a.qsh = d.q_stride_h * es;
     a.osb = d.o_stride_b * es; a.ost = d.o_stride_t * es; a.osh = d.o_stride_h * es;
-    const long long units = (long long)d.B * d.Hkv * w.n_split;
-    const dim3 grid((unsigned)((units + 7) / 8 * 8 * w.row_blocks));
-    const TreeForm f = tree_form(d);
+    const long long units = (long long)d.B * d.Hkv * w.n_split, even = (units * w.row_blocks + 7) / 8, by_unit = (units + 7) / 8 * w.row_blocks;
+    a.per_xcd = by_unit > even + even / 8 ? (int)even : 0;
+    const dim3 grid((unsigned)(8 * (a.per_xcd ? even : by_unit)));
+    int n_forms;
+    const TreeForm &f = tree_forms(d, n_forms)[w.form];
 #define LVLM_TREE(DT_, HD_, RB_, KW_)                                                                                      \
     if (d.dtype == DT_ && d.hd == HD_ && f.rb == RB_ && f.kw == KW_)                                                       \
         LVLM_LAUNCH(prof, (tree_attn_kernel<DT_, HD_, RB_, KW_>), grid, dim3(256), 0, prof.stream, a);
@@ -884,7 +921,8 @@ hipError_t launch_tree_attn(const Prof &prof, const lvlm_tree_desc &d, const Tre
     LVLM_TREE(LVLM_F32, 128, 1, 2)
     LVLM_TREE(LVLM_F32, 128, 1, 1)
     LVLM_TREE(LVLM_F32, 64, 1, 4)
-    LVLM_TREE(LVLM_F32, 64, 2, 1)
+    LVLM_TREE(LVLM_F32, 64, 1, 2)
+    LVLM_TREE(LVLM_F32, 64, 1, 1)
     prof.end();
 #undef LVLM_TREE
     if (w.n_split > 1) {
