@@ -451,8 +451,9 @@ LVLM_API lvlm_status lvlm_decode_attn_static(lvlm_ctx *ctx, void *stream, const 
  *   k, v      [n_pages, page_size, hd]        score, kind, orig_pos  [n_pages, page_size]
  *   pages     [B, Hkv, Lmax / page_size] i32  slot s of head (b, g) is place s % page_size of page
  *                                             pages[b][g][s / page_size]
- * Only table places below a head's length (the new one, when appending) are read.  A page number outside [0, n_pages)
- * holds nothing: entries written there are dropped, entries read there are not seen, and no memory is touched. */
+ * The whole table has to be readable; what it says at places from a head's length on (the new one, when appending) comes to
+ * nothing.  A page number outside [0, n_pages) holds nothing: entries written there are dropped, entries read there are
+ * not seen, and no memory is touched. */
 typedef struct {
     void *k, *v;
     float *score;         /* score, kind, orig_pos may be NULL: then they are not kept      */
@@ -501,7 +502,7 @@ typedef struct {          /* HOST struct of device pointers                     
  * pairs, of axis a by the sections, turns by the angle pos[a][b][t] * inv_freq[c],
  *   x_i' = x_i cos - x_j sin,  x_j' = x_j cos + x_i sin,
  * angles reduced in 64 bits (exact at any 32-bit position), products in fp32, one rounding to the dtype; channels from
- * rot_dim on, and values, are copied.  q_out[b][t] for t < n; rows from n on are neither read nor written.
+ * rot_dim on, and values, are copied.  q_out[b][t] for t < n; rows from n on (all T have to be readable) are not written.
  * A head whose entries do not all fit (len + n > Lmax, or a negative len) takes none of them and keeps its length: a caller
  * that cannot rule this out compares the lengths.  Without turning and with counts per head the call packs compressed lists,
  * with their score, kind and orig_pos, into pages.  len_out may be len itself.  q needs counts per sequence (n_stride_h 0) and

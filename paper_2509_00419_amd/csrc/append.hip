@@ -3,6 +3,8 @@
 #include "mma.h"
 #include "pages.h"
 
+#include <algorithm>
+
 namespace lvlm {
 namespace {
 
@@ -24,44 +26,46 @@ struct AppendArgs {
     int rot, adjacent, new_kind;
     int end0, end1;                         // first pair of the second and the third axis
     int tok_shift;                          // log2 of the tokens of a workgroup
+    int eager;                              // rows are asked for before it is known that they are in use
     int publish;                            // the workgroup that holds a head's tokens writes its new length
     long long ksb, kst, ksh, vsb, vst, vsh, qsb, qst, qsh, osb, ost, osh;   // bytes
     long long nsb, nsh, msb, msh;
 };
 
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
 // 16 channels of a row: two runs of eight.
 template <int DT>
 struct Piece {
     static constexpr int NV = 16 * esize<DT>() / 16;    // 16-byte words
-    uint4 w[NV];
+    u32x4 w[NV];
     __device__ __forceinline__ void load(const char *p, int lo, int hi) {
 #pragma unroll
         for (int i = 0; i < NV / 2; ++i) {
-            w[i] = *reinterpret_cast<const uint4 *>(p + lo + 16 * i);
-            w[NV / 2 + i] = *reinterpret_cast<const uint4 *>(p + hi + 16 * i);
+            w[i] = *reinterpret_cast<const u32x4 *>(p + lo + 16 * i);
+            w[NV / 2 + i] = *reinterpret_cast<const u32x4 *>(p + hi + 16 * i);
         }
     }
     __device__ __forceinline__ void store(char *p, int lo, int hi) const {
 #pragma unroll
         for (int i = 0; i < NV / 2; ++i) {
-            *reinterpret_cast<uint4 *>(p + lo + 16 * i) = w[i];
-            *reinterpret_cast<uint4 *>(p + hi + 16 * i) = w[NV / 2 + i];
+            *reinterpret_cast<u32x4 *>(p + lo + 16 * i) = w[i];
+            *reinterpret_cast<u32x4 *>(p + hi + 16 * i) = w[NV / 2 + i];
         }
     }
     __device__ __forceinline__ float get(int e) const {
-        const uint32_t *u = reinterpret_cast<const uint32_t *>(w);
-        if constexpr (DT == LVLM_F32) return __uint_as_float(u[e]);
-        return __uint_as_float((e & 1) ? u[e >> 1] & 0xffff0000u : u[e >> 1] << 16);
+        if constexpr (DT == LVLM_F32) return __uint_as_float(w[e >> 2][e & 3]);
+        const uint32_t u = w[e >> 3][(e >> 1) & 3];
+        return __uint_as_float((e & 1) ? u & 0xffff0000u : u << 16);
     }
     __device__ __forceinline__ void put(int e, float x0, float x1) {    // elements e (even), e + 1
-        uint32_t *u = reinterpret_cast<uint32_t *>(w);
         if constexpr (DT == LVLM_F32) {
-            u[e] = __float_as_uint(x0);
-            u[e + 1] = __float_as_uint(x1);
+            w[e >> 2][e & 3] = __float_as_uint(x0);
+            w[e >> 2][(e & 3) + 1] = __float_as_uint(x1);
         } else {
             typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
             typedef float f2 __attribute__((ext_vector_type(2)));
-            u[e >> 1] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x0, x1}, bf2));
+            w[e >> 3][(e >> 1) & 3] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{x0, x1}, bf2));
         }
     }
     // pairs: adjacent (2c, 2c + 1), or (c, 8 + c)
@@ -93,7 +97,15 @@ __device__ __forceinline__ bool fits(const AppendArgs &a, int len, int n) { retu
 // token's heads with them.  A row of keys or queries passes as 16-byte words, those of eight (hd 128) or four (hd 64) threads
 // next to each other.  Angles: position times frequency in 64 bits, a 31-bit by a 24-bit number and so all but exact, in
 // turns; what is left of the whole turns goes to fp32, where a turn is off by 2^-25 at most, whatever the position.
-template <int DT, int HD>
+//
+// What bounds it: a long call the memory (a row in, a row out), a short one its trips to memory.  A head's rows, its length
+// and what is known of its entries are asked for a head ahead, the first one's before the angles, so a short call waits for
+// two trips (rows and lengths, then the page) and the stores: one token 4.0 us, sixteen trees of
+// 32 tokens 5.8 us (18.8 with each head's loads after the angles and after its count).  A call that fills the chip more than
+// once takes several heads to a thread, which spreads the angles (16512 tokens of 56 heads: 125 us or 4.3 TB/s, 165 with one
+// head to a thread), and waits for a head's count before its rows, as rows that are not in use would pass for nothing (512 heads
+// of 472 to 1888 entries: 135 us or 4.7 TB/s; 171 with every row of the T read).
+template <int DT, int HD, bool TURNS>
 __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
     constexpr int ES = esize<DT>();
     constexpr int TPT = HD / 16;            // threads per token
@@ -104,10 +116,37 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
     const int t = blockIdx.x * toks + (slot & (toks - 1));
     const int b = blockIdx.z;
     const int u0 = blockIdx.y * lanes * a.per_thread + (slot >> a.tok_shift);
-    const bool turns = 16 * s < a.rot;
+    const bool turns = TURNS && 16 * s < a.rot;
     // the thread's two runs of eight channels, in bytes
-    const int lo = (turns && !a.adjacent ? 8 * s : 16 * s) * ES;
-    const int hi = turns && !a.adjacent ? lo + (a.rot / 2) * ES : lo + 8 * ES;
+    const bool halves = turns ? !a.adjacent : !TURNS;
+    const int lo = (halves ? 8 * s : 16 * s) * ES;
+    const int hi = halves ? lo + (TURNS ? a.rot / 2 : HD / 2) * ES : lo + 8 * ES;
+    struct Unit {
+        Piece<DT> x, y;                     // keys and values, or queries
+        int n, len, orig;
+        float score;
+        uint8_t kind;
+    };
+    auto ask = [&](int u, Unit &w) __attribute__((always_inline)) {   
+        if (t >= a.T || u >= a.units) return;
+        w.n = new_rows(a, b, u < a.Hkv ? u : 0);
+        if (!a.eager && t >= w.n) return;
+        if (u >= a.Hkv) {
+            w.x.load(a.q + b * a.qsb + t * a.qst + (u - a.Hkv) * a.qsh, lo, hi);
+            return;
+        }
+        w.len = a.len[b * a.Hkv + u];
+        w.x.load(a.k + b * a.ksb + t * a.kst + u * a.ksh, lo, hi);
+        w.y.load(a.v + b * a.vsb + t * a.vst + u * a.vsh, lo, hi);
+        if (s == 0) {
+            const long long m = b * a.msb + u * a.msh + t;
+            w.score = a.score ? a.score[m] : 0.f;
+            w.kind = a.kind ? a.kind[m] : (uint8_t)a.new_kind;
+            w.orig = a.orig ? a.orig[m] : a.pos ? a.pos[(long long)b * a.T + t] : t;
+        }
+    };
+    Unit w{};
+    ask(u0, w);
     float cs[8], sn[8];
     if (turns && t < a.T) {
         float freq[8];
@@ -127,31 +166,23 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
     for (int i = 0; i < a.per_thread; ++i) {
         const int u = u0 + i * lanes;
         if (u >= a.units) break;
-        if (u >= a.Hkv) {                   // a query head
-            const int h = u - a.Hkv;
-            if (t >= new_rows(a, b, 0)) continue;
-            Piece<DT> x;
-            x.load(a.q + b * a.qsb + t * a.qst + h * a.qsh, lo, hi);
-            if (turns) x.turn(cs, sn, a.adjacent);
-            x.store(a.qo + b * a.osb + t * a.ost + h * a.osh, lo, hi);
-            continue;
+        const bool query = u >= a.Hkv, in = t < a.T && t < w.n && (query || fits(a, w.len, w.n));
+        const long long row = in && !query ? a.at.row(b * a.Hkv + u, w.len + t) : -1;
+        Unit next{};
+        if (i + 1 < a.per_thread) ask(u + lanes, next);
+        if (turns) w.x.turn(cs, sn, a.adjacent);
+        if (query) {
+            if (in) w.x.store(a.qo + b * a.osb + t * a.ost + (u - a.Hkv) * a.osh, lo, hi);
+        } else if (row >= 0) {
+            w.x.store(a.ck + row * ROWB, lo, hi);
+            w.y.store(a.cv + row * ROWB, lo, hi);
+            if (s == 0) {
+                if (a.c_score) a.c_score[row] = w.score;
+                if (a.c_kind) a.c_kind[row] = w.kind;
+                if (a.c_orig) a.c_orig[row] = w.orig;
+            }
         }
-        const int hg = b * a.Hkv + u, n = new_rows(a, b, u), len = a.len[hg];
-        if (t >= n || !fits(a, len, n)) continue;
-        const long long row = a.at.row(hg, len + t);
-        if (row < 0) continue;
-        Piece<DT> x, y;
-        x.load(a.k + b * a.ksb + t * a.kst + u * a.ksh, lo, hi);
-        y.load(a.v + b * a.vsb + t * a.vst + u * a.vsh, lo, hi);
-        if (s == 0) {
-            const long long m = b * a.msb + u * a.msh + t;
-            if (a.c_score) a.c_score[row] = a.score ? a.score[m] : 0.f;
-            if (a.c_kind) a.c_kind[row] = a.kind ? a.kind[m] : (uint8_t)a.new_kind;
-            if (a.c_orig) a.c_orig[row] = a.orig ? a.orig[m] : a.pos ? a.pos[(long long)b * a.T + t] : t;
-        }
-        if (turns) x.turn(cs, sn, a.adjacent);
-        x.store(a.ck + row * ROWB, lo, hi);
-        y.store(a.cv + row * ROWB, lo, hi);
+        w = next;
     }
     if (!a.publish || blockIdx.x != 0) return;
     __syncthreads();                        // (in place: everybody has read the head's length)
@@ -269,20 +300,28 @@ hipError_t launch_kv_append(const Prof &prof, const lvlm_append_desc &d, const l
     const int lanes = slots >> a.tok_shift, tok_blocks = (d.T + (1 << a.tok_shift) - 1) >> a.tok_shift;
     const int rounds = (a.units + lanes - 1) / lanes;
     const long long all = (long long)tok_blocks * d.B * rounds;     // workgroups if every thread took one unit
-    a.per_thread = (int)(all / 4096 < 1 ? 1 : all / 4096 > 16 ? 16 : all / 4096);
-    const int groups = (rounds + a.per_thread - 1) / a.per_thread;
+    const bool turns = d.rot_dim > 0;
+    const long long wanted = std::max(1ll, std::min(all / 4096, 16ll));
+    const int groups = (int)((rounds + wanted - 1) / wanted);
+    a.per_thread = (rounds + groups - 1) / groups;
+    a.eager = wanted == 1;
     const bool in_place = len_out == len;
     a.publish = tok_blocks == 1 || !in_place;
     if (tok_blocks > 0) {
         prof.begin("kv_append");
         const dim3 grid(tok_blocks, groups, d.B);
-        if (d.dtype == LVLM_BF16) {
-            if (d.hd == 128) LVLM_LAUNCH(prof, (kv_append_kernel<LVLM_BF16, 128>), grid, dim3(256), 0, prof.stream, a);
-            else LVLM_LAUNCH(prof, (kv_append_kernel<LVLM_BF16, 64>), grid, dim3(256), 0, prof.stream, a);
-        } else {
-            if (d.hd == 128) LVLM_LAUNCH(prof, (kv_append_kernel<LVLM_F32, 128>), grid, dim3(256), 0, prof.stream, a);
-            else LVLM_LAUNCH(prof, (kv_append_kernel<LVLM_F32, 64>), grid, dim3(256), 0, prof.stream, a);
-        }
+#define LVLM_APPEND(DT_, HD_, TURNS_)                        \
+    if (d.dtype == DT_ && d.hd == HD_ && turns == TURNS_)    \
+        LVLM_LAUNCH(prof, (kv_append_kernel<DT_, HD_, TURNS_>), grid, dim3(256), 0, prof.stream, a);
+        LVLM_APPEND(LVLM_BF16, 128, true)
+        LVLM_APPEND(LVLM_BF16, 128, false)
+        LVLM_APPEND(LVLM_BF16, 64, true)
+        LVLM_APPEND(LVLM_BF16, 64, false)
+        LVLM_APPEND(LVLM_F32, 128, true)
+        LVLM_APPEND(LVLM_F32, 128, false)
+        LVLM_APPEND(LVLM_F32, 64, true)
+        LVLM_APPEND(LVLM_F32, 64, false)
+#undef LVLM_APPEND
         prof.end();
     }
     if (tok_blocks == 0 ? !in_place : !a.publish) {
