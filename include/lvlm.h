@@ -513,7 +513,8 @@ LVLM_API lvlm_status lvlm_kv_append(lvlm_ctx *ctx, void *stream, const lvlm_appe
 typedef struct {
     int32_t dtype;     /* LVLM_BF16 or LVLM_F32: q, caches, out                             */
     int32_t B, T;      /* sequences, drafted rows per sequence at most: 1 .. 1024           */
-    int32_t Hq, Hkv;   /* query heads, KV heads (Hq % Hkv == 0, Hq / Hkv * T < 65536)       */
+    int32_t Hq, Hkv;   /* query heads, KV heads (Hq % Hkv == 0, Hq / Hkv * T < 65536);      */
+                       /* B * Hq * T < 2^31, B * Hkv * ceil(Hq / Hkv * T / 128) < 2^23      */
     int32_t hd;        /* 64 or 128                                                         */
     int32_t Lmax;      /* that of the cache                                                 */
     int32_t len_bound; /* host-known upper bound of every len (0 = Lmax); sizes the launch  */
@@ -543,7 +544,7 @@ LVLM_API lvlm_status lvlm_tree_mask(int T, const int32_t *parent, uint32_t *mask
 
 typedef struct {
     int32_t dtype;     /* LVLM_BF16 or LVLM_F32                                             */
-    int32_t B, Hkv;
+    int32_t B, Hkv;    /* sequences, KV heads; B * Hkv < 2^23                               */
     int32_t hd;        /* 64 or 128                                                         */
     int32_t P;         /* places of path per sequence: 1 .. 65536                           */
     int32_t reserved;  /* 0                                                                 */

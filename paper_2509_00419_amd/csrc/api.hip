@@ -33,6 +33,7 @@ int elem_bytes(int dt) { return dt == LVLM_BF16 ? 2 : 4; }
 // Upper limits of the size fields (include/lvlm.h states them): generous for any cache or sequence that fits a GPU,
 // and tight enough that no size or grid computation in the library can overflow.
 constexpr int kMaxBatch = 1 << 16, kMaxHeads = 1 << 10, kMaxTokens = 1 << 22, kMaxSlots = 1 << 24, kMaxRowElems = 1 << 20;
+constexpr long long kMaxGroups = 1 << 23;   // workgroups of one launch: half of what a grid of 256 threads each may have
 const char *kTooLarge = "size beyond the documented limits (B 65536, heads 1024, N 4194304, Lmax 16777216, row_elems 1048576)";
 
 const char *check_score(const lvlm_score_desc *d) {
@@ -277,6 +278,8 @@ const char *check_tree(const lvlm_tree_desc *d) {
     if (d->T < 1 || d->T > 1024) return "T must be in [1, 1024]";
     if ((long long)(d->Hq / d->Hkv) * d->T >= 65536) return "query rows per KV head (Hq/Hkv * T) must be below 65536";
     if ((long long)d->B * d->Hq * d->T >= (1ll << 31)) return "query rows (B * Hq * T) must be below 2^31";
+    if ((long long)d->B * d->Hkv * ((d->Hq / d->Hkv * d->T + 127) / 128) >= kMaxGroups)
+        return "groups of 128 query rows (B * Hkv * ceil(Hq / Hkv * T / 128)) must be below 2^23";
     if (d->len_bound < 0 || d->len_bound > d->Lmax) return "len_bound must be in [0, Lmax]";
     if (!(d->scale > 0.0f) || !(d->scale < INFINITY)) return "scale must be positive and finite";
     const int vec = 16 / elem_bytes(d->dtype);
@@ -291,6 +294,7 @@ const char *check_commit(const lvlm_commit_desc *d) {
     if (d->reserved != 0) return "reserved fields must be 0";
     if (d->B < 1 || d->Hkv < 1) return "sizes must be positive";
     if (d->B > kMaxBatch - 1 || d->Hkv > kMaxHeads) return kTooLarge;
+    if ((long long)d->B * d->Hkv >= kMaxGroups) return "lists (B * Hkv) must be below 2^23";
     if (d->P < 1 || d->P > 65536) return "P must be in [1, 65536]";
     return nullptr;
 }

@@ -859,7 +859,7 @@ TreeWs tree_ws(const lvlm_tree_desc &d) {
         for (int wanted : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             if (wanted > steps) break;
             const long long run = (steps + wanted - 1) / wanted, split = (steps + run - 1) / run;
-            if (pairs * blocks * split >= (1ll << 27)) break;
+            if (pairs * blocks * split >= (1ll << 23) || (split > 1 && pairs > 65535)) break;     // a launch's most (the fold's: by pairs)
             const double per_unit = (double)(pairs * blocks * split) / kUnits, whole = (double)((pairs * blocks * split + kUnits - 1) / kUnits);
             const double rounds = per_unit > 8 ? per_unit : whole;
             double t = (f.workgroup + f.tile * (double)(run * f.tps)) * (rounds <= 1 ? 1.0 : rounds * f.shared);

@@ -93,7 +93,7 @@ def test_tree_attention_refuses(kw, word):
 
 @pytest.mark.parametrize("kw,word", [
     (dict(hd=96), "head dimension"), (dict(dtype=2), "dtype"), (dict(B=0), "positive"), (dict(Hkv=2000), "limits"), (dict(P=0), "P must"),
-    (dict(P=65537), "P must"), (dict(reserved=1), "reserved"), (dict(path=None), "null"), (dict(path=TAB + 1), "aligned"),
+    (dict(P=65537), "P must"), (dict(B=8192, Hkv=1024), "2^23"), (dict(reserved=1), "reserved"), (dict(path=None), "null"), (dict(path=TAB + 1), "aligned"),
     (dict(len_out=None), "null"), (dict(len_out=LEN + 8), "overlaps len"), (dict(cache={"k": None}), "null"),
 ])
 def test_commit_refuses(kw, word):
@@ -115,14 +115,22 @@ def test_struct_sizes_match_the_header_layout():
     assert C.sizeof(bd.CommitDesc) == 6 * 4
 
 
-def test_workspace_query_answers_at_the_limits_and_refuses_beyond():
-    ctx = lv.Context(0)
-    for B, T, Hq, Hkv, Lmax in ((65535, 1024, 1024, 1024, 1 << 24), (1, 1, 1, 1, 1), (1, 1024, 63, 1, 1 << 24), (65535, 1, 1024, 16, 1 << 24)):
-        for dtype in (bd.BF16, bd.F32):
-            assert ctx.workspace_bytes(bd.OP_TREE_ATTN, bd.TreeDesc(dtype, B, T, Hq, Hkv, 128, Lmax, 0, 0.1, 0, T * Hq * 128, Hq * 128, 128,
-                                                                    T * Hq * 128, Hq * 128, 128)) >= 0
-    with pytest.raises(lv.LvlmError):
-        ctx.workspace_bytes(bd.OP_TREE_ATTN, bd.TreeDesc(bd.BF16, 1, 1, 1, 1, 128, 1 << 25, 0, 0.1, 0, 128, 128, 128, 128, 128, 128))
+def _tree_ws(dtype, B, T, Hq, Hkv, Lmax, hd=128):
+    return lv.Context(0).workspace_bytes(bd.OP_TREE_ATTN, bd.TreeDesc(dtype, B, T, Hq, Hkv, hd, Lmax, 0, 0.1, 0, T * Hq * hd, Hq * hd, hd,
+                                                                      T * Hq * hd, Hq * hd, hd))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("dtype", [bd.BF16, bd.F32])
+def test_workspace_query_answers_at_the_limits_and_refuses_beyond(dtype, hd):
+    for B, T, Hq, Hkv, Lmax in ((1, 1, 1, 1, 1), (1, 1024, 63, 1, 1 << 24), (65535, 1, 64, 64, 1 << 24), (8191, 1, 1024, 1024, 1 << 24),
+                                (1023, 1024, 1024, 1024, 1 << 24), (65535, 128, 64, 2, 1 << 24)):
+        assert _tree_ws(dtype, B, T, Hq, Hkv, Lmax, hd) >= 0
+    assert _tree_ws(dtype, 65535, 1, 2, 2, 1 << 24, hd) == 0     # (more lists than the launch that folds takes: one run each)
+    for B, T, Hq, Hkv, Lmax, word in ((65535, 1024, 1024, 1024, 1 << 24, "2\\^31"), (8192, 1, 1024, 1024, 1, "2\\^23"),
+                                      (65535, 1, 1024, 256, 64, "2\\^23"), (1, 1, 1, 1, 1 << 25, "limits")):
+        with pytest.raises(lv.LvlmError, match=word):
+            _tree_ws(dtype, B, T, Hq, Hkv, Lmax, hd)
 
 
 def test_tensors_of_another_device_type_or_layout_are_refused():
