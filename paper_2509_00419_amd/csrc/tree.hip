@@ -60,7 +60,7 @@ struct TreeShape {
     // Steps in LDS (piped: a step's keys are read a step before its values and travel a step ahead of them).  Two workgroups share a
     // compute unit where two steps each leave room for it.
     static constexpr int RING = PIPED ? (HD == 128 ? 4 : 8) : 2 * STEPB > (64 << 10) ? 2 : (64 << 10) / STEPB > 4 ? 4 : (64 << 10) / STEPB;
-    static constexpr int REACH = PIPED ? RING : RING - 1;       // the step that is fetched next (piped: of keys), from the one in hand
+    static constexpr int REACH = RING - 1;      // the step that is fetched next (piped: of keys; of values the one before), from the one in hand
     static constexpr int OPEN = PIPED ? RING - 3 : RW == 1 ? RING - 1 : RING - 2;       // steps still travelling when it is waited for
     static constexpr int PER_CU = DT == LVLM_BF16 && !PIPED && RING * STEPB <= (64 << 10) ? 2 : 1;     // workgroups to a compute unit
     static constexpr int PITCH = HD * 4 + 16;           // of a row of sums put together in LDS
@@ -416,10 +416,10 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
             l[x] += weigh(s[x], m[x] == -INFINITY ? 0.f : m[x]);
         }
         // A value that is no number must not reach the rows that do not see it -- their weight for it is 0, and 0 times it is
-        // not: in a tile that has any they are left out of the product, and added to the rows that do see them.  (One row, or
-        // none of the drafts in the tile: nothing is unseen but what repeats the last entry.)
+        // not: in a tile that has any they are left out of the product, and added to the rows that do see them.  (A repeat of
+        // the last entry is not seen either.)
         bool odd = false;
-        if (nowhere || (d < 32 && n > 1)) {
+        if (in != ~0u || (d < 32 && n > 1)) {
             // the largest exponent of all (in bf16 of both halves of a word)
             typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
             u16x2 top2 = {0, 0};
@@ -475,12 +475,13 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
     };
 
     // Step s is next: it has landed (piped: and the next step's keys), and the step at REACH is under way.  (Before step 0: only
-    // the latter.)  Careful, piped: the keys of step s are needed too, so theirs is not the place to fill yet.
+    // the latter.)  A slot is filled again when nobody reads it any more: its values after its own step, its keys, piped, a step
+    // earlier -- but those of step 0 are read in step 0, so the keys too keep a step's distance.
     int fetched = 0;                                // steps this wave has asked for
     auto fetch_to = [&](int last) __attribute__((always_inline)) {
         if (fetched <= last && fetched < n_steps) fetch(fetched++);
     };
-    auto turn = [&](int s, bool careful) __attribute__((always_inline)) {
+    auto turn = [&](int s) __attribute__((always_inline)) {
         if constexpr (RW == 1) {
             // the slot about to be filled was read for the step before: those reads have to be back
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
@@ -491,11 +492,10 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
         } else {
             // everybody's parts have landed, and everybody's reads of the steps before are back
             if (s >= 0) {
-                if (fetched < n_steps && !(Z::PIPED && careful)) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NL * TPS * Z::OPEN) : "memory");
+                if (fetched < n_steps) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(NL * TPS * Z::OPEN) : "memory");
                 else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
             }
-            if constexpr (Z::PIPED) fetch_to(s + Z::REACH - (rw >= RW / 2 ? 2 : careful ? 1 : 0));
-            else fetch_to(s + Z::REACH);
+            fetch_to(s + Z::REACH - (Z::PIPED && rw >= RW / 2 ? 1 : 0));
         }
     };
 
@@ -583,7 +583,7 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
             stage(values_at(s, 0), keys_at(s + 1, 1), sb, sa, pb, pa);
             if (++s >= n_steps) break;
             taken = tile_of(s, 1) >= n_clear;
-            turn(s, taken);
+            turn(s);
             if (taken) break;
         }
         const char *vt = values_at(s + RING - 1, 1);
@@ -618,15 +618,15 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
             // values of the step before the first: zero, as are their probabilities
             char *none = lds + values_slot(RING - 1, TPS - 1);
             for (int i = 64 * rw + lane; i < TILEB / 16; i += 64 * RW) *reinterpret_cast<uint4 *>(none + 16 * i) = make_uint4(0, 0, 0, 0);
-            for (; s < 0; ++s) turn(s, false);
+            for (; s < 0; ++s) turn(s);
             if (n_steps > 0) {
                 const bool clear = tile_of(0, TPS - 1) < n_clear;
-                turn(0, !clear);
+                turn(0);
                 turned = clear && !idle ? clear_run(s) : true;
             }
         } else {
             for (; s < n_steps; ++s) {
-                turn(s, false);
+                turn(s);
                 if (s < 0) continue;
                 if (tile_of(s, 0) >= n_clear) {
                     turned = true;
@@ -637,18 +637,26 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
         }
         for (; s < n_steps; ++s) {
             __builtin_assume(s >= 0);
-            if (!turned) turn(s, true);
+            if (!turned) turn(s);
             turned = false;
 #pragma unroll 1
             for (int u = 0; u < TPS; ++u)
                 if (tile_of(s, u) < n_tiles && !idle) careful_tile(s, u, std::false_type{});
         }
     }
-    // A row whose sum ran away from its reference (or is no number): the whole workgroup begins again, and rescales on the way.
+    // A row whose sum ran away from its reference (or is no number), or took a product beyond fp32: the whole workgroup begins
+    // again, and rescales on the way.
     {
         bool risk = false;
 #pragma unroll
-        for (int x = 0; x < RB; ++x) risk |= !(l[x] < __builtin_amdgcn_exp2f(kRiskTree));
+        for (int x = 0; x < RB; ++x) {
+            uint32_t top = 0;
+#pragma unroll
+            for (int cb = 0; cb < NCB; ++cb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) top = max(top, __float_as_uint(o[x][cb][r]) & 0x7fffffffu);
+            risk |= !(l[x] < __builtin_amdgcn_exp2f(kRiskTree)) || top >= 0x7f800000u;
+        }
         risk = __builtin_amdgcn_ballot_w64(risk) != 0ull && !idle;
         if (lane == 0) again_s[wave] = risk;
     }
@@ -656,7 +664,7 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
     if (__builtin_expect(again_s[0] | again_s[1] | again_s[2] | again_s[3], 0)) {
         begin();
         for (int s = -Z::REACH; s < n_steps; ++s) {
-            turn(s, true);
+            turn(s);
             if (s < 0) continue;
 #pragma unroll 1
             for (int u = 0; u < TPS; ++u)

@@ -228,6 +228,137 @@ def test_one_row_is_decode_attention(ctx):
     assert (out[:, 0] - ref).abs().max() <= 1e-5
 
 
+# Shapes that take every way a call is cut: 32, 64, 128 and 256 rows to a workgroup, with the entries whole and in runs, over more
+# steps than travel at a time.
+LONG = [
+    # dtype, B, T, Hq, Hkv, d, slots, page
+    (BF, 33, 70, 8, 8, 64, 200, 0), (BF, 9, 130, 8, 1, 64, 4200, 0), (BF, 33, 40, 8, 8, 64, 200, 0), (BF, 5, 40, 14, 1, 64, 4200, 0),
+    (BF, 33, 70, 14, 2, 64, 1100, 0), (BF, 33, 70, 14, 2, 64, 1024, 64), (BF, 9, 70, 14, 1, 64, 4200, 0), (BF, 9, 70, 14, 1, 64, 4096, 256),
+    (BF, 33, 40, 8, 4, 128, 200, 0), (BF, 9, 130, 14, 1, 128, 2100, 0), (BF, 33, 11, 16, 4, 128, 1100, 0), (BF, 5, 40, 8, 8, 128, 4096, 16),
+    (BF, 9, 500, 14, 1, 128, 600, 0), (BF, 9, 500, 14, 1, 128, 768, 32), (BF, 5, 1000, 2, 1, 128, 4200, 0), (BF, 9, 333, 16, 8, 128, 1100, 0),
+    (FP, 9, 130, 14, 1, 64, 200, 0), (FP, 1, 1, 2, 1, 64, 1100, 0), (FP, 33, 11, 16, 4, 64, 200, 0), (FP, 1, 1, 2, 1, 64, 4200, 0),
+    (FP, 33, 1, 8, 4, 64, 1024, 32), (FP, 33, 40, 8, 4, 128, 200, 0), (FP, 33, 40, 2, 1, 128, 608, 32), (FP, 33, 130, 2, 2, 128, 1100, 0),
+]
+
+
+def dense(c, q, n_rows, mask):
+    """The formula in 64 bits with whole matrices, a head at a time on the GPU: out, lse, sum of p |v|; rows not in use are NaN."""
+    B, T, Hq, d = q.shape
+    H = c.len.shape[1]
+    G = Hq // H
+    out, weight = (torch.full((B, T, Hq, d), float("nan"), dtype=torch.float64, device=DEV) for _ in range(2))
+    lse = torch.full((B, Hq, T), float("nan"), dtype=torch.float64, device=DEV)
+    kf, vf = c.k.flatten(0, -2), c.v.flatten(0, -2)
+    room = c.k.shape[2] if c.pages is None else c.pages.shape[2] * c.k.shape[1]
+    for b in range(B):
+        n = T if n_rows is None else n_rows[b]
+        for g in range(H):
+            L = int(c.len[b, g])
+            s = torch.arange(L, device=DEV)
+            rows = s + (b * H + g) * room if c.pages is None else c.pages[b, g, s // c.k.shape[1]].long() * c.k.shape[1] + s % c.k.shape[1]
+            k, v = kf[rows].double(), vf[rows].double()
+            sees = torch.ones(n, L, dtype=torch.bool, device=DEV)
+            sees[:, L - n:] = torch.ones(n, n, device=DEV).tril().bool() if mask is None else mask[b, :n, :n]
+            for h in range(g * G, g * G + G):
+                z = (q[b, :n, h].double() @ k.t().contiguous() * d ** -0.5).masked_fill(~sees, float("-inf"))
+                lse[b, h, :n] = torch.logsumexp(z, -1)
+                p = torch.softmax(z, -1)
+                out[b, :n, h], weight[b, :n, h] = p @ v, p @ v.abs()
+    return out, lse, weight
+
+
+def against_dense(ctx, c, q, dtype, n_rows, parents, clean=None, but=None):
+    """One call against the formula (of the caches `clean`, without drafted row `but`, if given)."""
+    B, T, Hq, d = q.shape
+    words = mask = None
+    if parents is not None:
+        words = lv.tree_mask(torch.from_numpy(np.stack(parents))).to(DEV)
+        mask = torch.from_numpy(np.stack([O.tree_mask(p) for p in parents])).to(DEV)
+    rows = None if n_rows is None else torch.tensor(n_rows, dtype=torch.int32, device=DEV)
+    out = torch.full((B, T, Hq, d), 7.0, dtype=dtype, device=DEV)
+    lse = torch.full((B, Hq, T), 7.0, device=DEV)
+    ctx.tree_attn(q, c.k, c.v, c.len, mask=words, n_rows=rows, pages=c.pages, out=out, row_lse=lse)
+    clean = clean or c
+    ref, ref_lse, weight = dense(clean, q, n_rows, mask)
+    if but is not None:
+        assert not bool(torch.isfinite(out[:, but].float()).all())
+        ref[:, but], ref_lse[:, :, but], out[:, but], lse[:, :, but] = float("nan"), float("nan"), 7.0, 7.0
+    e = (d + 4) * U * float(q.abs().double().sum(-1).max() * clean.k.abs().max().double()) * d ** -0.5
+    n = int(c.len.max())
+    tol = weight * (2 * e + (n + 8) * U) + 1e-30
+    if dtype == BF:
+        tol = tol + 2.0 ** -8 * (weight + ref.abs())
+    unused = torch.isnan(ref)
+    assert bool((out[unused] == 7.0).all()) and bool((lse[torch.isnan(ref_lse)] == 7.0).all())
+    off = ((out.double() - ref).abs() / tol)[~unused]
+    assert bool((off <= 1.0).all()), float(off.max())
+    off = ((lse.double() - ref_lse).abs() - (e + (n + 4) * U + 4 * U * ref_lse.abs()))[~torch.isnan(ref_lse)]
+    assert bool((off <= 0.0).all()), float(off.max())
+    return out, lse
+
+
+@pytest.mark.parametrize("dtype,B,T,Hq,Hkv,d,slots,page", LONG)
+def test_every_cut_matches_the_formula(ctx, dtype, B, T, Hq, Hkv, d, slots, page):
+    seed = B * T + slots
+    r = np.random.default_rng(seed)
+    n_rows = [T] + r.integers(1, T + 1, B - 1).tolist()
+    most = slots - T
+    lens = np.array(n_rows)[:, None] + np.where(r.random((B, Hkv)) < 0.5, most, r.integers(0, most + 1, (B, Hkv)))
+    c = Caches(dtype, lens.tolist(), slots, d, page, seed).dev()
+    q = torch.randn(B, T, Hq, d, generator=torch.Generator().manual_seed(seed)).to(dtype).to(DEV)
+    parents = [tree_of(T, seed + b) for b in range(B)] if seed % 2 else None
+    against_dense(ctx, c, q, dtype, n_rows, parents)
+
+
+@pytest.mark.parametrize("dtype,B,T,Hq,Hkv,d,slots,page", LONG)
+def test_every_cut_survives_logits_that_grow_and_values_that_are_large(ctx, dtype, B, T, Hq, Hkv, d, slots, page):
+    """Along the entries the logits rise by 300 (beyond any fixed reference), then by 40 with values near the end of the type, where
+    sums relative to the first entries would overflow."""
+    g = torch.Generator().manual_seed(slots)
+    c = Caches(dtype, [[slots] * Hkv] * B, slots, d, page, slots).dev()
+    rise = (torch.randn(slots, d, generator=g) * 0.01 + torch.linspace(0, 1, slots)[:, None]).to(dtype).to(DEV)
+    s = torch.arange(slots, device=DEV)
+    for b in range(B):
+        for h in range(Hkv):
+            if page:
+                c.k[c.pages[b, h, s // page].long(), s % page] = rise
+            else:
+                c.k[b, h] = rise
+    for gain, large in ((300.0, 1.0), (40.0, 1e30)):
+        c.v.mul_(large)
+        against_dense(ctx, c, torch.full((B, T, Hq, d), gain / d ** 0.5, device=DEV).to(dtype), dtype, None, None)
+
+
+@pytest.mark.parametrize("dtype,T,Hq,d,slots", [(BF, 1000, 2, 128, 4200), (BF, 70, 14, 64, 4200), (FP, 40, 2, 128, 608), (BF, 130, 8, 64, 4200)])
+def test_no_cut_lets_in_what_a_row_does_not_see(ctx, dtype, T, Hq, d, slots):
+    """NaN and infinities in the keys and values of one drafted row, and behind the last entry."""
+    B = 9
+    c = Caches(dtype, [[slots - 37]] * B, slots, d, 0, slots).dev()
+    q = torch.randn(B, T, Hq, d, generator=torch.Generator().manual_seed(T)).to(dtype).to(DEV)
+    parents = [np.array([-1] + [0] * (T - 1), dtype=np.int32)] * B           # siblings: each sees row 0 and itself
+    clean = c.dev()
+    clean.k, clean.v = c.k.clone(), c.v.clone()
+    c.k[:, :, slots - 37:], c.v[:, :, slots - 37:] = float("nan"), float("inf")
+    against_dense(ctx, c, q, dtype, None, parents, clean)
+    at = slots - 37 - T + T // 2
+    for bad_k, bad_v in ((float("nan"), float("nan")), (0.0, float("inf"))):
+        c.k[:, :, at], c.v[:, :, at] = bad_k, bad_v
+        against_dense(ctx, c, q, dtype, None, parents, clean, T // 2)
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("L", [1, 40, 97, 256])
+def test_an_infinite_value_gives_an_infinity_and_no_nan(ctx, dtype, L):
+    """The last entry, seen by the one row and repeated in the rest of its tile."""
+    c = Caches(dtype, [[L]], 256, 64, 0, L).dev()
+    c.v[0, 0, L - 1, ::2] = float("inf")
+    c.v[0, 0, L - 1, 1::4] = float("-inf")
+    q = torch.randn(1, 1, 2, 64, generator=torch.Generator().manual_seed(L)).to(dtype).to(DEV)
+    out, _ = ctx.tree_attn(q, c.k, c.v, c.len)
+    assert bool((out[..., ::2] == float("inf")).all()) and bool((out[..., 1::4] == float("-inf")).all())
+    assert bool(torch.isfinite(out[..., 3::4].float()).all())
+
+
 # ---- append ---------------------------------------------------------------------------------------------------------
 
 
