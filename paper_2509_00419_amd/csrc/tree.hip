@@ -743,6 +743,153 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
     }
 }
 
+// fp32, up to four rows (MR: their number, rounded up to a power of two): the matrix cores' tiles would be mostly empty, and a product
+// of theirs in fp32 takes as long for one row as for 32.  An entry's row goes to HD / 4 lanes, four channels each: dot products
+// on the vector ALUs, summed over those lanes, and every group of lanes keeps maxima, sums and sums of p v of its own until the
+// end.  A wave takes EPW entries (of one page) at a time and asks for the next ones before it works on these; eight waves
+// share a run of entries.  What bounds it is the memory's latency in short lists, its rate in many of them.  Against the matrix
+// cores' forms, us: 4 lists of 256 entries of 64 channels, one row 9.2 -> 4.1, two 9.4 -> 5.7, four 9.1 -> 8.4 (eight rows: 9.6, not
+// 13.2); 64 x 4096 35 -> 24 (one row; 5.5 TB/s), 35 -> 29 (four); 128 channels 16 x 1024 17.6 -> 9.9, 64 x 4096 95 -> 44.
+template <int HD, int MR>
+__global__ __launch_bounds__(512) void tree_few_kernel(TreeArgs a) {
+    constexpr int WAVES = 8, LPE = HD / 4, GROUPS = 64 / LPE, U = 4, EPW = GROUPS * U, STEP = WAVES * EPW, ROWB = HD * 4;
+    static_assert(16 % EPW == 0, "a wave's entries lie in one page");
+    __shared__ float4 o_s[WAVES][MR][LPE];
+    __shared__ float m_s[WAVES][MR], l_s[WAVES][MR];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int li = lane % LPE, gi = lane / LPE;
+    const int pairs = a.B * a.Hkv, unit = blockIdx.x;
+    if (unit >= pairs * a.n_split) return;
+    const int split = unit / pairs, pair = unit % pairs, b = pair / a.Hkv, g = pair % a.Hkv;
+    const int len = uniform_word(a.len + pair), n = rows_in_use(a, b), n_live = n * a.G;
+    const int L = min(max(len, 0), a.bound), s_lo = split * a.split_len, s_hi = min(L, s_lo + a.split_len);
+    if (n_live == 0 || (s_lo >= s_hi && a.n_split > 1)) return;
+    const int first = max(len, 0) - n;
+
+    struct Entries {
+        float4 k[U], v[U];
+        int nowhere;                                // they lie in no page
+    };
+    auto first_of = [&](int step) { return s_lo + step * STEP + wave * EPW; };
+    auto ask = [&](int step, Entries &e) __attribute__((always_inline)) {
+        const int j0 = first_of(step);
+        if (j0 >= s_hi) return;
+        long long r0 = (long long)pair * a.at.Lmax + j0;
+        e.nowhere = 0;
+        if (a.at.pages) {
+            const int page = uniform_word(a.at.pages + (long long)pair * a.at.per_head + (j0 >> a.at.shift));
+            e.nowhere = (unsigned)page >= (unsigned)a.at.n_pages;
+            r0 = e.nowhere ? 0 : ((long long)page << a.at.shift) + (j0 & ((1 << a.at.shift) - 1));
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {               // (past the last entry that one again)
+            const long long at = (r0 + min(GROUPS * u + gi, s_hi - 1 - j0)) * ROWB + 16 * li;
+            e.k[u] = *reinterpret_cast<const float4 *>(a.k + at);
+            e.v[u] = *reinterpret_cast<const float4 *>(a.v + at);
+        }
+    };
+    Entries now{}, next{};
+    ask(0, now);
+    float4 q[MR], o[MR];
+    float m[MR], l[MR];
+    uint32_t drafts[MR];                            // that a row sees
+#pragma unroll
+    for (int r = 0; r < MR; ++r) {
+        const int row = min(r, n_live - 1), t = row / a.G;
+        q[r] = *reinterpret_cast<const float4 *>(a.q + b * a.qsb + t * a.qst + (long long)(g * a.G + row - t * a.G) * a.qsh + 16 * li);
+        q[r] = make_float4(q[r].x * a.scale_log2, q[r].y * a.scale_log2, q[r].z * a.scale_log2, q[r].w * a.scale_log2);
+        drafts[r] = a.mask ? (uint32_t)uniform_word(reinterpret_cast<const int32_t *>(a.mask) + (long long)b * a.T + t) : (2u << t) - 1u;
+        m[r] = -INFINITY;
+        l[r] = 0.f;
+        o[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    auto weigh = [&](const Entries &e, int j0, auto all_tag) __attribute__((always_inline)) {
+        constexpr bool ALL = decltype(all_tag)::value;      // every row sees all of them
+#pragma unroll
+        for (int r = 0; r < MR; ++r) {
+            float s[U], top = m[r];
+            bool sees[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                s[u] = fmaf(q[r].x, e.k[u].x, fmaf(q[r].y, e.k[u].y, fmaf(q[r].z, e.k[u].z, q[r].w * e.k[u].w)));
+                s[u] += dpp_quad1(s[u]);
+                s[u] += dpp_quad2(s[u]);
+                s[u] += dpp_half_mirror(s[u]);
+                s[u] += dpp_row_mirror(s[u]);
+                if (LPE == 32) s[u] += swap_rows(s[u]);
+                const int j = j0 + GROUPS * u + gi;
+                sees[u] = ALL || (j < s_hi && !e.nowhere && (j < first || (drafts[r] >> (j - first) & 1u)));
+                if (!sees[u]) s[u] = -INFINITY;
+                top = fmaxf(top, s[u]);
+            }
+            const float ref = top == -INFINITY ? 0.f : top, f = __builtin_amdgcn_exp2f(m[r] - ref);
+            m[r] = top;
+            l[r] *= f;
+            o[r] = make_float4(o[r].x * f, o[r].y * f, o[r].z * f, o[r].w * f);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float p = __builtin_amdgcn_exp2f(s[u] - ref);
+                l[r] += p;
+                const float4 v = ALL || sees[u] ? e.v[u] : make_float4(0.f, 0.f, 0.f, 0.f);     // (0 times what it holds may be no 0)
+                o[r] = make_float4(fmaf(p, v.x, o[r].x), fmaf(p, v.y, o[r].y), fmaf(p, v.z, o[r].z), fmaf(p, v.w, o[r].w));
+            }
+        }
+    };
+    for (int step = 0; first_of(step) < s_hi; ++step) {
+        const int j0 = first_of(step);
+        ask(step + 1, next);
+        if (j0 + EPW <= min(first, s_hi) && !now.nowhere) weigh(now, j0, std::true_type{});
+        else weigh(now, j0, std::false_type{});
+        now = next;
+    }
+    // the groups of a wave meet, then the waves
+#pragma unroll
+    for (int r = 0; r < MR; ++r) {
+        float top = fmaxf(m[r], swap_halves(m[r]));
+        if (LPE == 16) top = fmaxf(top, swap_rows(top));
+        const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[r] - top);
+        float x[5] = {o[r].x * f, o[r].y * f, o[r].z * f, o[r].w * f, l[r] * f};
+#pragma unroll
+        for (int i = 0; i < 5; ++i) {
+            x[i] += swap_halves(x[i]);
+            if (LPE == 16) x[i] += swap_rows(x[i]);
+        }
+        if (gi == 0) o_s[wave][r][li] = make_float4(x[0], x[1], x[2], x[3]);
+        if (lane == 0) {
+            m_s[wave][r] = top;
+            l_s[wave][r] = x[4];
+        }
+    }
+    __syncthreads();
+    const int row = tid / LPE;
+    if (row >= min(n_live, MR)) return;
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) top = fmaxf(top, m_s[w][row]);
+    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_s[w][row] - top);
+        const float4 x = o_s[w][row][tid % LPE];
+        sum = fmaf(l_s[w][row], f, sum);
+        y = make_float4(fmaf(x.x, f, y.x), fmaf(x.y, f, y.y), fmaf(x.z, f, y.z), fmaf(x.w, f, y.w));
+    }
+    const int t = row / a.G, h = g * a.G + row - t * a.G;
+    char *dst;
+    if (a.n_split > 1) {
+        const long long at = ((long long)pair * a.n_split + split) * a.M + row;
+        if (tid % LPE == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(top, sum);
+        dst = reinterpret_cast<char *>(a.part_o) + at * ROWB;
+    } else {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;
+        y = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+        if (tid % LPE == 0 && a.row_lse)
+            a.row_lse[((long long)b * a.Hq + h) * a.T + t] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * (1.f / kLog2e);
+        dst = a.out + b * a.osb + t * a.ost + h * a.osh;
+    }
+    *reinterpret_cast<float4 *>(dst + 16 * (tid % LPE)) = y;
+}
+
 // Folds the runs of a pair's entries: a row to HD / 4 threads, four channels each.  Lane i of them looks at run i (and further ones):
 // the maxima and sums of all runs come in one round trip, the sums of p v eight runs at a time.
 template <int DT, int HD>
@@ -827,13 +974,16 @@ __global__ __launch_bounds__(256) void tree_fold_kernel(TreeArgs a) {
 // 128, us: 4 pairs x 28 rows x 512 entries of 128 channels 12.6 -> 7.8, 8 x 384 x 2048 35 -> 17, 32 x 384 x 512 32 -> 13, 64 x 1 x
 // 2048 23 -> 16, 128 x 192 x 2048 72 -> 44, 512 x 768 x 128 117 -> 70; with 256 rows where they are right 32 x 384 x 16384
 // 160 -> 134.
+constexpr int kFewRows = 4;
+int few_rows(long long M) { return M <= 1 ? 1 : M <= 2 ? 2 : kFewRows; }
 struct TreeForm {
     int rb, kw, tps;        // blocks of 32 rows to a wave; waves side by side over entries; tiles of a wave in a step
     float workgroup, tile;  // us: a workgroup without entries; a tile of 32 entries in one of its waves
     float shared;           // workgroups that share a compute unit, of what they would take in turn (1: they do not share)
     float alone;            // bytes per us that a workgroup gets from memory (1.6 times as many where the cache holds all entries)
     float busy;             // us of a compute unit for a tile of one row block, on a chip that has all it can do
-    int rows() const { return 32 * rb * (4 / kw); }
+    int rows() const { return rb == 0 ? kFewRows : 32 * rb * (4 / kw); }     // (rb 0: fp32, few rows on the vector ALUs; a workgroup takes 0.6 us more for each,
+                                                                        // a tile as long again)
 };
 constexpr int kTreeForms = 4;
 const TreeForm *tree_forms(const lvlm_tree_desc &d, int &n) {
@@ -842,10 +992,11 @@ const TreeForm *tree_forms(const lvlm_tree_desc &d, int &n) {
          {1, 1, 1, 3.7f, 0.69f, 0.62f, 8.5e3f, 0.11f}, {2, 1, 2, 8.9f, 0.58f, 1.f, 92e3f, 0.74f}},
         {{1, 4, 1, 4.2f, 0.77f, 1.f, 53e3f, 0.14f}, {1, 2, 1, 3.9f, 0.69f, 0.81f, 20e3f, 0.39f},
          {1, 1, 1, 4.5f, 0.82f, 0.62f, 14.5e3f, 0.68f}, {2, 1, 2, 8.6f, 0.92f, 1.f, 92e3f, 0.71f}}};
-    static constexpr TreeForm kF32[2][3] = {
-        {{1, 4, 1, 4.1f, 2.8f, 1.f, 34e3f, 0.78f}, {1, 2, 1, 4.3f, 2.5f, 1.f, 14e3f, 1.5f}, {1, 1, 1, 4.4f, 2.4f, 1.f, 29e3f, 2.8f}},
-        {{1, 2, 1, 5.7f, 5.0f, 1.f, 52e3f, 2.8f}, {1, 1, 1, 6.9f, 4.4f, 1.f, 56e3f, 5.3f}, {}}};
-    n = d.dtype == LVLM_BF16 ? kTreeForms : d.hd == 64 ? 3 : 2;
+    static constexpr TreeForm kF32[2][kTreeForms] = {
+        {{0, 4, 1, 3.3f, 0.25f, 0.6f, 50e3f, 0.05f}, {1, 4, 1, 4.1f, 2.8f, 1.f, 34e3f, 0.78f}, {1, 2, 1, 4.3f, 2.5f, 1.f, 14e3f, 1.5f},
+         {1, 1, 1, 4.4f, 2.4f, 1.f, 29e3f, 2.8f}},
+        {{0, 2, 1, 3.3f, 0.25f, 0.6f, 50e3f, 0.05f}, {1, 2, 1, 5.7f, 5.0f, 1.f, 52e3f, 2.8f}, {1, 1, 1, 6.9f, 4.4f, 1.f, 56e3f, 5.3f}, {}}};
+    n = d.dtype == LVLM_BF16 || d.hd == 64 ? kTreeForms : 3;
     return d.dtype == LVLM_BF16 ? kBf16[d.hd == 128] : kF32[d.hd == 128];
 }
 
@@ -862,6 +1013,9 @@ TreeWs tree_ws(const lvlm_tree_desc &d) {
     double best = 0;
     for (int i = 0; i < n_forms; ++i) {
         const TreeForm &f = forms[i];
+        if (f.rb == 0 && M > kFewRows) continue;
+        const float begin = f.rb == 0 ? f.workgroup + 0.6f * (float)(few_rows(M) - 1) : f.workgroup;
+        const float tile = f.rb == 0 ? f.tile * (float)(few_rows(M) + 1) : f.tile;
         const int step = 32 * f.kw * f.tps;
         const long long blocks = (M + f.rows() - 1) / f.rows(), steps = ((long long)bound + step - 1) / step;
         for (int wanted : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
@@ -870,9 +1024,9 @@ TreeWs tree_ws(const lvlm_tree_desc &d) {
             if (pairs * blocks * split >= (1ll << 23) || (split > 1 && pairs > 65535)) break;     // a launch's most (the fold's: by pairs)
             const double per_unit = (double)(pairs * blocks * split) / kUnits, whole = (double)((pairs * blocks * split + kUnits - 1) / kUnits);
             const double rounds = per_unit > 8 ? per_unit : whole;
-            double t = (f.workgroup + f.tile * (double)(run * f.tps)) * (rounds <= 1 ? 1.0 : rounds * f.shared);
-            t = std::max(t, f.workgroup + (double)std::min<long long>(run * step, bound) * d.hd * es * 2 / (f.alone * (bytes > 200e6 ? 1.0 : 1.6)));
-            t = std::max(t, f.workgroup + std::max(bytes / 14e6, tiles * f.busy) * (double)blocks);      // 14 TB/s from the L2s
+            double t = (begin + tile * (double)(run * f.tps)) * (rounds <= 1 ? 1.0 : rounds * f.shared);
+            t = std::max(t, begin + (double)std::min<long long>(run * step, bound) * d.hd * es * 2 / (f.alone * (bytes > 200e6 ? 1.0 : 1.6)));
+            t = std::max(t, begin + std::max(bytes / 14e6, tiles * f.busy) * (double)blocks);      // 14 TB/s from the L2s
             t = std::max(t, 1.0 + bytes / 7e6);                                                          // ... 7 from memory
             if (split > 1) t += 6.0 + (double)pairs * split * M * d.hd * 8 / 5.5e6;
             if (w.n_split == 0 || t < best) {
@@ -931,8 +1085,18 @@ hipError_t launch_tree_attn(const Prof &prof, const lvlm_tree_desc &d, const Tre
     LVLM_TREE(LVLM_F32, 64, 1, 4)
     LVLM_TREE(LVLM_F32, 64, 1, 2)
     LVLM_TREE(LVLM_F32, 64, 1, 1)
-    prof.end();
 #undef LVLM_TREE
+    const int few = f.rb == 0 ? few_rows(a.M) : 0;
+#define LVLM_FEW(HD_, MR_)                                                                                                 \
+    if (d.hd == HD_ && few == MR_) LVLM_LAUNCH(prof, (tree_few_kernel<HD_, MR_>), grid, dim3(512), 0, prof.stream, a);
+    LVLM_FEW(64, 1)
+    LVLM_FEW(64, 2)
+    LVLM_FEW(64, 4)
+    LVLM_FEW(128, 1)
+    LVLM_FEW(128, 2)
+    LVLM_FEW(128, 4)
+#undef LVLM_FEW
+    prof.end();
     if (w.n_split > 1) {
         const int rows = 256 / (d.hd / 4);
         const dim3 fold((unsigned)((a.M + rows - 1) / rows), (unsigned)(d.B * d.Hkv));

@@ -228,7 +228,7 @@ def test_one_row_is_decode_attention(ctx):
     assert (out[:, 0] - ref).abs().max() <= 1e-5
 
 
-# Shapes that take every way a call is cut: 32, 64, 128 and 256 rows to a workgroup, with the entries whole and in runs, over more
+# Shapes that take every way a call is cut: up to 4 (fp32), 32, 64, 128 and 256 rows to a workgroup, with the entries whole and in runs, over more
 # steps than travel at a time.
 LONG = [
     # dtype, B, T, Hq, Hkv, d, slots, page
@@ -238,6 +238,9 @@ LONG = [
     (BF, 9, 500, 14, 1, 128, 600, 0), (BF, 9, 500, 14, 1, 128, 768, 32), (BF, 5, 1000, 2, 1, 128, 4200, 0), (BF, 9, 333, 16, 8, 128, 1100, 0),
     (FP, 9, 130, 14, 1, 64, 200, 0), (FP, 1, 1, 2, 1, 64, 1100, 0), (FP, 33, 11, 16, 4, 64, 200, 0), (FP, 1, 1, 2, 1, 64, 4200, 0),
     (FP, 33, 1, 8, 4, 64, 1024, 32), (FP, 33, 40, 8, 4, 128, 200, 0), (FP, 33, 40, 2, 1, 128, 608, 32), (FP, 33, 130, 2, 2, 128, 1100, 0),
+    (FP, 1, 1, 8, 1, 64, 600, 0), (FP, 1, 1, 8, 1, 64, 4200, 0), (FP, 16, 1, 14, 2, 64, 1100, 0), (FP, 33, 1, 32, 4, 128, 200, 0),
+    (FP, 1, 1, 8, 1, 128, 200, 0), (FP, 2, 4, 2, 2, 64, 200, 0), (FP, 3, 3, 4, 4, 64, 4096, 16), (FP, 2, 4, 3, 3, 128, 2048, 64),
+    (FP, 5, 1, 4, 4, 128, 96, 0), (FP, 33, 2, 8, 8, 128, 1100, 0), (FP, 2, 1, 4, 4, 64, 37, 0),
 ]
 
 
@@ -329,7 +332,8 @@ def test_every_cut_survives_logits_that_grow_and_values_that_are_large(ctx, dtyp
         against_dense(ctx, c, torch.full((B, T, Hq, d), gain / d ** 0.5, device=DEV).to(dtype), dtype, None, None)
 
 
-@pytest.mark.parametrize("dtype,T,Hq,d,slots", [(BF, 1000, 2, 128, 4200), (BF, 70, 14, 64, 4200), (FP, 40, 2, 128, 608), (BF, 130, 8, 64, 4200)])
+@pytest.mark.parametrize("dtype,T,Hq,d,slots", [(BF, 1000, 2, 128, 4200), (BF, 70, 14, 64, 4200), (FP, 40, 2, 128, 608), (BF, 130, 8, 64, 4200),
+                                             (FP, 2, 2, 64, 4200), (FP, 4, 1, 128, 608), (FP, 3, 1, 64, 200)])
 def test_no_cut_lets_in_what_a_row_does_not_see(ctx, dtype, T, Hq, d, slots):
     """NaN and infinities in the keys and values of one drafted row, and behind the last entry."""
     B = 9
