@@ -160,9 +160,10 @@ struct AttnWs {
 AttnWs attn_ws(const lvlm_attn_desc &d);
 
 struct TreeWs {
-    size_t part_o, part_ml, total;
+    size_t part_o, part_ml, places, total;
     int form;                   // which kernel: rows of a workgroup
-    int n_split, split_len;     // runs of a pair's entries (split_len each), folded by a second launch
+    int n_split, run;           // runs of a pair's entries (run each), folded by a second launch
+    int dealt, step;            // ... dealt out by the lengths, n_split to a pair on average (multiples of step)
     int row_blocks;             // workgroups a pair's rows take
 };
 TreeWs tree_ws(const lvlm_tree_desc &d);

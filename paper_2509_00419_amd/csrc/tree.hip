@@ -20,11 +20,13 @@ struct TreeArgs {
     float *row_lse;
     const int32_t *len, *n_rows;
     const uint32_t *mask;
-    float *part_o;      // [pair][split][row][HD]  sums of p v, relative to the split's maximum
-    float *part_ml;     // [pair][split][row][2]   that maximum (logits times scale, base 2) and the sum of p
+    float *part_o;      // [run][row][HD]  sums of p v, relative to the split's maximum
+    float *part_ml;     // [run][row][2]   that maximum (logits times scale, base 2) and the sum of p
     CachePlace at;
     int B, T, Hq, Hkv, G, words, bound, M;      // M: T * G rows to a pair
-    int n_split, split_len, row_blocks, per_xcd;
+    int n_split, run, row_blocks, per_xcd;      // runs to a pair (run entries each)
+    int dealt, step;                            // ... on average, dealt out by the lengths (multiples of step)
+    int2 *places;                               // [pair] dealt: its first place, its runs
     float scale_log2;
     long long qsb, qst, qsh, osb, ost, osh;     // bytes
 };
@@ -42,6 +44,94 @@ __device__ __forceinline__ const char *uniform_ptr(const char *p) {
 // Rows of a pair: row = t * G + head; those of t < n_rows[b] are in use.
 __device__ __forceinline__ int rows_in_use(const TreeArgs &a, int b) {
     return a.n_rows ? min(max(uniform_word(a.n_rows + b), 0), a.T) : a.T;
+}
+
+// Runs of entries, long calls: a head's length is its own and only the GPU knows it, so the pairs' entries are dealt out there.  Every
+// run is as long as it has to be for all of them to fit pairs * n_split places; the first places go to the first pair's runs, and so
+// on.  Each wave works this out for itself, 64 pairs at a time, which takes it 1 us.  16 sequences x 8 heads of 128 channels and 128
+// rows in 16384 slots, against runs of 4096 slots each, us: all of them in use 234 -> 238, a quarter 163 -> 75, 200 to 16384 by head
+// (few long ones) 174 -> 85, one sequence full and the others 500 133 -> 42; 8192 to 16384 by head 236 -> 225.
+constexpr int kSharePairs = 512, kShareRuns = 64;   // pairs at most; runs of one pair at most (that the fold takes)
+struct Share {
+    static constexpr int CHUNKS = kSharePairs / 64;
+    int pairs, run;                                 // entries of a run
+    float L[CHUNKS];                                // of pair 64 c + lane
+    // runs that L entries make (1 / run is off by half a step, the product by another: the floor is one too low at most)
+    __device__ __forceinline__ int runs(float l) const {
+        const int all = (int)l;
+        int n = (int)(l * (1.f / (float)run));
+        if (n * run < all) ++n;
+        return n * run < all ? n + 1 : n;
+    }
+    __device__ __forceinline__ Share(const TreeArgs &a) : pairs(a.B * a.Hkv) {
+        const int lane = threadIdx.x & 63;
+        float total = 0.f, most = 0.f;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+            if (64 * c < pairs) {
+                const int i = 64 * c + lane;
+                L[c] = i < pairs ? (float)min(max(a.len[i], 0), a.bound) : 0.f;
+                total += L[c];
+                most = fmaxf(most, L[c]);
+            }
+        total = wave_sum(total);
+        most = wave_max(most);
+        const float places = (float)(pairs * a.n_split);
+        run = max((int)ceilf(fmaxf(total / places, most * (1.f / kShareRuns))), 1);
+        run = (run + a.step - 1) / a.step * a.step;
+        for (;;) {                                  // (ends: runs as long as the longest pair are one to a pair)
+            float n = 0.f;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+                if (64 * c < pairs) n += (float)runs(L[c]);
+            if (wave_sum(n) <= places) break;
+            run += max(run / (16 * a.step), 1) * a.step;
+        }
+        run = __builtin_amdgcn_readfirstlane(run);
+    }
+    // the pair and the run of a place (pair -1: it stays empty)
+    __device__ __forceinline__ void find(int place, int &pair, int &split, int &used) const {
+        const int lane = threadIdx.x & 63;
+        int before = 0;
+        pair = -1;
+        split = used = 0;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c)
+            if (64 * c < pairs && pair < 0) {
+                const int n = runs(L[c]);
+                int upto = n;                       // runs of the chunk's pairs up to this one
+#pragma unroll
+                for (int d = 1; d < 64; d *= 2) {
+                    const int x = __shfl_up(upto, d);
+                    if (lane >= d) upto += x;
+                }
+                const unsigned long long beyond = __builtin_amdgcn_ballot_w64(before + upto > place);
+                if (beyond != 0ull) {
+                    const int at = __builtin_ctzll(beyond);
+                    pair = 64 * c + at;
+                    used = __builtin_amdgcn_readlane(n, at);
+                    split = place - before - (__builtin_amdgcn_readlane(upto, at) - used);
+                }
+                before += __builtin_amdgcn_readlane(upto, 63);
+            }
+    }
+};
+
+// The run a workgroup works on, and its place among the parts.  Neighbours belong to different pairs, so that what is slow in a run
+// (drafts, in the last one of a pair) does not gather on one XCD (512 rows, 8 pairs of 16896 entries: 292 us, not 255).
+struct Run {
+    int pair, place, from, len;                     // (pair -1: none)
+};
+__device__ __forceinline__ Run run_of(const TreeArgs &a, int unit, bool first_rows) {
+    const int pairs = a.B * a.Hkv;
+    int pair = __builtin_amdgcn_readfirstlane(unit % pairs), split = __builtin_amdgcn_readfirstlane(unit / pairs);
+    const int place = pair * a.n_split + split;
+    if (!a.dealt) return {pair, place, split * a.run, a.run};
+    const Share share(a);
+    int used;
+    share.find(place, pair, split, used);
+    if (pair >= 0 && split == 0 && first_rows && threadIdx.x == 0) a.places[pair] = make_int2(place, used);
+    return {pair, place, split * share.run, share.run};
 }
 
 constexpr float kLazyTree = 8.f;    // careful tiles: log2 of how far a row's maximum may run ahead of the reference before a rescale
@@ -120,12 +210,14 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
     const int item = a.per_xcd ? xcd * a.per_xcd + seq : (seq / a.row_blocks * 8 + xcd) * a.row_blocks + seq % a.row_blocks;
     const int unit = item / a.row_blocks;
     if (unit >= pairs * a.n_split || (a.per_xcd && seq >= a.per_xcd)) return;
-    const int split = __builtin_amdgcn_readfirstlane(unit / pairs), pair = __builtin_amdgcn_readfirstlane(unit % pairs);
+    const Run at_run = run_of(a, unit, item % a.row_blocks == 0);
+    const int pair = at_run.pair;
+    if (pair < 0) return;
     const int b = pair / a.Hkv, g = pair % a.Hkv;
     const int row0 = (item % a.row_blocks) * Z::ROWS;
     const int len = uniform_word(a.len + pair), n = rows_in_use(a, b), n_live = n * a.G;
     const int L = min(max(len, 0), a.bound);
-    const int s_lo = split * a.split_len, s_hi = min(L, s_lo + a.split_len);
+    const int s_lo = at_run.from, s_hi = min(L, s_lo + at_run.len);
     if (row0 >= n_live || (s_lo >= s_hi && a.n_split > 1)) return;
     const int first = max(len, 0) - n;              // entry of drafted row 0 (below 0: the head holds fewer than n)
     const int n_tiles = s_hi > s_lo ? (s_hi - s_lo + 31) >> 5 : 0;
@@ -697,7 +789,7 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
             for (int w = 0; w < KW; ++w) sum = fmaf(l_s[w * RW + rw][l32], __builtin_amdgcn_exp2f(m_s[w * RW + rw][l32] - ref), sum);
         }
         const int head = g * a.G + row - t_row[x] * a.G;
-        const long long at = ((long long)pair * a.n_split + split) * a.M + row;
+        const long long at = (long long)at_run.place * a.M + row;
         if (a.n_split == 1) f = sum == 0.f ? 0.f : f / sum;
         if (kw == 0 && hf == 0 && shown) {
             if (a.n_split > 1) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(top, sum);
@@ -760,9 +852,12 @@ __global__ __launch_bounds__(512) void tree_few_kernel(TreeArgs a) {
     const int li = lane % LPE, gi = lane / LPE;
     const int pairs = a.B * a.Hkv, unit = blockIdx.x;
     if (unit >= pairs * a.n_split) return;
-    const int split = unit / pairs, pair = unit % pairs, b = pair / a.Hkv, g = pair % a.Hkv;
+    const Run at_run = run_of(a, unit, true);
+    const int pair = at_run.pair;
+    if (pair < 0) return;
+    const int b = pair / a.Hkv, g = pair % a.Hkv;
     const int len = uniform_word(a.len + pair), n = rows_in_use(a, b), n_live = n * a.G;
-    const int L = min(max(len, 0), a.bound), s_lo = split * a.split_len, s_hi = min(L, s_lo + a.split_len);
+    const int L = min(max(len, 0), a.bound), s_lo = at_run.from, s_hi = min(L, s_lo + at_run.len);
     if (n_live == 0 || (s_lo >= s_hi && a.n_split > 1)) return;
     const int first = max(len, 0) - n;
 
@@ -877,7 +972,7 @@ __global__ __launch_bounds__(512) void tree_few_kernel(TreeArgs a) {
     const int t = row / a.G, h = g * a.G + row - t * a.G;
     char *dst;
     if (a.n_split > 1) {
-        const long long at = ((long long)pair * a.n_split + split) * a.M + row;
+        const long long at = (long long)at_run.place * a.M + row;
         if (tid % LPE == 0) *reinterpret_cast<float2 *>(a.part_ml + at * 2) = make_float2(top, sum);
         dst = reinterpret_cast<char *>(a.part_o) + at * ROWB;
     } else {
@@ -897,11 +992,16 @@ __global__ __launch_bounds__(256) void tree_fold_kernel(TreeArgs a) {
     constexpr int ES = esize<DT>(), TPR = HD / 4, PER = 64 / TPR, AT_ONCE = 8;      // threads per row; runs per lane
     const int pair = blockIdx.y, b = pair / a.Hkv, g = pair % a.Hkv;
     const int li = threadIdx.x % TPR, c = 4 * li, row = blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-    const int n_live = rows_in_use(a, b) * a.G, L = min(max(uniform_word(a.len + pair), 0), a.bound);
+    const int n_live = rows_in_use(a, b) * a.G;
     if ((int)blockIdx.x * (256 / TPR) >= n_live) return;
-    const int used = (L + a.split_len - 1) / a.split_len;
+    const int L = min(max(uniform_word(a.len + pair), 0), a.bound);
+    int place = pair * a.n_split, used = (L + a.run - 1) / a.run;
+    if (a.dealt && L > 0) {
+        place = a.places[pair].x;
+        used = a.places[pair].y;
+    }
     const bool live = row < n_live;
-    const long long at = (long long)pair * a.n_split * a.M + min(row, n_live - 1);
+    const long long at = (long long)place * a.M + min(row, n_live - 1);
     float m[PER], w[PER], top = -INFINITY;
 #pragma unroll
     for (int x = 0; x < PER; ++x) {
@@ -975,6 +1075,7 @@ __global__ __launch_bounds__(256) void tree_fold_kernel(TreeArgs a) {
 // 2048 23 -> 16, 128 x 192 x 2048 72 -> 44, 512 x 768 x 128 117 -> 70; with 256 rows where they are right 32 x 384 x 16384
 // 160 -> 134.
 constexpr int kFewRows = 4;
+constexpr double kDealUs = 25;   // calls that take longer deal their runs out by the lengths
 int few_rows(long long M) { return M <= 1 ? 1 : M <= 2 ? 2 : kFewRows; }
 struct TreeForm {
     int rb, kw, tps;        // blocks of 32 rows to a wave; waves side by side over entries; tiles of a wave in a step
@@ -1029,18 +1130,23 @@ TreeWs tree_ws(const lvlm_tree_desc &d) {
             t = std::max(t, begin + std::max(bytes / 14e6, tiles * f.busy) * (double)blocks);      // 14 TB/s from the L2s
             t = std::max(t, 1.0 + bytes / 7e6);                                                          // ... 7 from memory
             if (split > 1) t += 6.0 + (double)pairs * split * M * d.hd * 8 / 5.5e6;
+            const bool dealt = split > 1 && pairs <= kSharePairs && t > kDealUs;
+            if (!dealt && t > kDealUs) t *= 1.1;    // (its lengths may be as uneven as they like)
             if (w.n_split == 0 || t < best) {
                 best = t;
                 w.form = i;
                 w.n_split = (int)split;
-                w.split_len = (int)(run * step);
+                w.run = (int)(run * step);
+                w.step = step;
+                w.dealt = dealt;
                 w.row_blocks = (int)blocks;
             }
         }
     }
     if (w.n_split > 1) {
         w.part_ml = align_up((size_t)(pairs * w.n_split * M) * d.hd * 4, 256);
-        w.total = w.part_ml + align_up((size_t)(pairs * w.n_split * M) * 8, 256);
+        w.places = w.part_ml + align_up((size_t)(pairs * w.n_split * M) * 8, 256);
+        w.total = w.places + (w.dealt ? align_up((size_t)pairs * 8, 256) : 0);
     }
     return w;
 }
@@ -1056,10 +1162,11 @@ hipError_t launch_tree_attn(const Prof &prof, const lvlm_tree_desc &d, const Tre
     a.row_lse = row_lse; a.len = len; a.n_rows = n_rows; a.mask = mask;
     a.part_o = reinterpret_cast<float *>(ws + w.part_o);
     a.part_ml = reinterpret_cast<float *>(ws + w.part_ml);
+    a.places = reinterpret_cast<int2 *>(ws + w.places);
     a.at = cache_place(c);
     a.B = d.B; a.T = d.T; a.Hq = d.Hq; a.Hkv = d.Hkv; a.G = d.Hq / d.Hkv; a.words = (d.T + 31) / 32; a.M = a.G * d.T;
     a.bound = d.len_bound > 0 ? d.len_bound : d.Lmax;
-    a.n_split = w.n_split; a.split_len = w.split_len; a.row_blocks = w.row_blocks;
+    a.n_split = w.n_split; a.run = w.run; a.dealt = w.dealt; a.step = w.step; a.row_blocks = w.row_blocks;
     a.scale_log2 = d.scale * kLog2e;
     a.qsb = d.q_stride_b * es; a.qst = d.q_stride_t * es; a.qsh = d.q_stride_h * es;
     a.osb = d.o_stride_b * es; a.ost = d.o_stride_t * es; a.osh = d.o_stride_h * es;

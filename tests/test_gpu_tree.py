@@ -332,6 +332,27 @@ def test_every_cut_survives_logits_that_grow_and_values_that_are_large(ctx, dtyp
         against_dense(ctx, c, torch.full((B, T, Hq, d), gain / d ** 0.5, device=DEV).to(dtype), dtype, None, None)
 
 
+@pytest.mark.parametrize("dtype,B,T,Hq,Hkv,d,slots", [(BF, 16, 32, 32, 8, 128, 4096), (BF, 33, 4, 16, 8, 128, 8192), (FP, 9, 2, 8, 8, 64, 8192),
+                                                       (BF, 3, 200, 8, 2, 128, 8192), (FP, 20, 9, 4, 4, 64, 2048)])
+def test_runs_dealt_out_by_the_lengths(ctx, dtype, B, T, Hq, Hkv, d, slots):
+    """Long calls share out what the heads hold: all of it, nothing, one long list among empty ones, anything between."""
+    r = np.random.default_rng(B)
+    q = torch.randn(B, T, Hq, d, generator=torch.Generator().manual_seed(T)).to(dtype).to(DEV)
+    c = Caches(dtype, [[slots] * Hkv] * B, slots, d, 0, B).dev()
+    for lens in (np.full((B, Hkv), slots), np.full((B, Hkv), T), np.where(np.arange(B * Hkv).reshape(B, Hkv) == B * Hkv // 2, slots, T),
+                 np.where(r.random((B, Hkv)) < 0.1, slots - 7, T + 1), T + (r.random((B, Hkv)) ** 3 * (slots - T)).astype(int)):
+        c.len = torch.from_numpy(lens.astype(np.int32)).to(DEV)
+        against_dense(ctx, c, q, dtype, None, None)
+    c.len = torch.zeros(B, Hkv, dtype=torch.int32, device=DEV)              # and nothing at all, but for one row in one head
+    c.len[B // 2, Hkv // 2] = 1
+    out, lse = ctx.tree_attn(q, c.k, c.v, c.len, want_lse=True)
+    G, h = Hq // Hkv, Hkv // 2
+    heads = slice(h * G, h * G + G)
+    assert torch.equal(out[B // 2, T - 1, heads], c.v[B // 2, h, :1].expand(G, d))
+    out[B // 2, T - 1, heads] = 0
+    assert not bool(out.any()) and int(torch.isfinite(lse).sum()) == G
+
+
 @pytest.mark.parametrize("dtype,T,Hq,d,slots", [(BF, 1000, 2, 128, 4200), (BF, 70, 14, 64, 4200), (FP, 40, 2, 128, 608), (BF, 130, 8, 64, 4200),
                                              (FP, 2, 2, 64, 4200), (FP, 4, 1, 128, 608), (FP, 3, 1, 64, 200)])
 def test_no_cut_lets_in_what_a_row_does_not_see(ctx, dtype, T, Hq, d, slots):
