@@ -252,6 +252,10 @@ const char *check_append(const lvlm_append_desc *d, const lvlm_append_src *s, co
     if (overlap(s->k, kb, c->k, cb) || overlap(s->k, kb, c->v, cb) || overlap(s->v, vb, c->k, cb) || overlap(s->v, vb, c->v, cb))
         return "new rows overlap the cache";
     if (overlap(c->k, cb, c->v, cb)) return "the cache's keys and values overlap";
+    const size_t slots = cache_bytes(*c, d->B, d->Hkv, 1), mn = span(d->B, 1, d->Hkv, T, d->m_stride_b, 0, d->m_stride_h, 1);
+    if (d->T > 0 && (overlap(s->score, s->score ? mn * 4 : 0, c->score, slots * 4) || overlap(s->kind, s->kind ? mn : 0, c->kind, slots) ||
+                     overlap(s->orig_pos, s->orig_pos ? mn * 4 : 0, c->orig_pos, slots * 4)))
+        return "new score, kind or orig_pos overlaps the cache's";
     if (s->q) {
         if ((why = check_rows(d->B, T, d->Hq, d->hd, d->q_stride_b, d->q_stride_t, d->q_stride_h, vec, false))) return why;
         if ((why = check_rows(d->B, T, d->Hq, d->hd, d->qo_stride_b, d->qo_stride_t, d->qo_stride_h, vec, true))) return why;
@@ -708,6 +712,10 @@ lvlm_status lvlm_kv_append(lvlm_ctx *ctx, void *stream, const lvlm_append_desc *
     if (!ctx) return LVLM_ERR_INVALID_ARG;
     if (const char *why = check_append(d, src, cache)) return fail(ctx, LVLM_ERR_INVALID_ARG, "kv_append: %s", why);
     if (const char *why = check_lengths(len, len_out, d->B, d->Hkv)) return fail(ctx, LVLM_ERR_INVALID_ARG, "kv_append: %s", why);
+    const size_t heads = (size_t)d->B * d->Hkv * 4;
+    if (overlap(src->n_new, span(d->B, 1, d->Hkv, 1, d->n_stride_b, 0, d->n_stride_h, 4), len_out, heads) ||
+        overlap(src->pos, (size_t)d->n_axes * d->B * d->T * 4, len_out, heads))
+        return fail(ctx, LVLM_ERR_INVALID_ARG, "kv_append: len_out overlaps n_new or pos");
     if (d->T == 0 && len == len_out) return LVLM_OK;
     const DeviceScope scope(ctx);
     if (lvlm_status st = scope.status(ctx)) return st;
@@ -730,6 +738,10 @@ lvlm_status lvlm_tree_attn(lvlm_ctx *ctx, void *stream, const lvlm_tree_desc *d,
     const size_t cb = cache_bytes(*cache, d->B, d->Hkv, (size_t)d->hd * eb);
     if (overlap(q, qb, out, ob) || overlap(cache->k, cb, out, ob) || overlap(cache->v, cb, out, ob))
         return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: out overlaps q or the cache");
+    const size_t lb = (size_t)d->B * d->Hq * d->T * 4;
+    if (row_lse && (overlap(row_lse, lb, q, qb) || overlap(row_lse, lb, out, ob) || overlap(row_lse, lb, cache->k, cb) ||
+                    overlap(row_lse, lb, cache->v, cb)))
+        return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: row_lse overlaps q, out or the cache");
     const TreeWs w = tree_ws(*d);
     if (lvlm_status st = need_ws(ctx, w.total)) return st;
     const DeviceScope scope(ctx);
@@ -746,6 +758,9 @@ lvlm_status lvlm_tree_commit(lvlm_ctx *ctx, void *stream, const lvlm_commit_desc
     if (const char *why = check_lengths(len, len_out, d->B, d->Hkv)) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_commit: %s", why);
     if (!path || !n_path) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_commit: null pointer");
     if (!aligned4(path) || !aligned4(n_path)) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_commit: path and n_path must be 4-byte aligned");
+    const size_t heads = (size_t)d->B * d->Hkv * 4;
+    if (overlap(path, (size_t)d->B * d->P * 4, len_out, heads) || overlap(n_path, (size_t)d->B * 4, len_out, heads))
+        return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_commit: len_out overlaps path or n_path");
     const DeviceScope scope(ctx);
     if (lvlm_status st = scope.status(ctx)) return st;
     return after_launch(ctx, launch_tree_commit(Prof{ctx, static_cast<hipStream_t>(stream)}, *d, *cache, len, path, n_path, len_out));

@@ -52,6 +52,9 @@ def _append(desc=(), src=(), cache=(), length=(LEN, LEN2)):
     (dict(cache={"pages": TAB, "page_size": 0, "n_pages": 1}), "power of two"),
     (dict(cache={"pages": TAB, "page_size": 512, "n_pages": 1}), "multiple of page_size"),
     (dict(cache={"pages": TAB, "page_size": 64, "n_pages": 0}), "n_pages"),
+    (dict(src={"n_new": LEN2}), "len_out overlaps n_new"), (dict(src={"pos": LEN2 + 8}), "len_out overlaps n_new or pos"),
+    (dict(src={"orig_pos": 1 << 20}, cache={"orig_pos": (1 << 20) + 16}), "overlaps the cache's"),
+    (dict(src={"kind": 1 << 20}, cache={"kind": 1 << 20}), "overlaps the cache's"),
     (dict(length=(None, LEN2)), "null"), (dict(length=(LEN, LEN + 4)), "overlaps len"), (dict(length=(LEN, LEN2 + 2)), "aligned"),
 ])
 def test_append_refuses(kw, word):
@@ -83,7 +86,7 @@ def _tree(desc=(), cache=(), q=Q, out=QO, length=LEN, n_rows=None, mask=MASK, ls
     (dict(desc={"q_stride_t": 1023}), "multiples"), (dict(desc={"o_stride_h": 64}), "overlap"), (dict(desc={"o_stride_t": 0}), "overlap"),
     (dict(desc={"Lmax": 128}), "differ"), (dict(q=None), "null"), (dict(out=None), "null"), (dict(length=None), "null"),
     (dict(q=Q + 4), "aligned"), (dict(length=LEN + 1), "aligned"), (dict(mask=MASK + 2), "aligned"), (dict(out=Q + 1024), "overlap"),
-    (dict(out=V + 1024), "overlap"), (dict(cache={"v": None}), "null"),
+    (dict(out=V + 1024), "overlap"), (dict(cache={"v": None}), "null"), (dict(lse=QO + 64), "row_lse overlaps"), (dict(lse=K), "row_lse overlaps"),
     (dict(cache={"pages": TAB, "page_size": 24, "n_pages": 3}), "power of two"),
 ])
 def test_tree_attention_refuses(kw, word):
@@ -94,7 +97,8 @@ def test_tree_attention_refuses(kw, word):
 @pytest.mark.parametrize("kw,word", [
     (dict(hd=96), "head dimension"), (dict(dtype=2), "dtype"), (dict(B=0), "positive"), (dict(Hkv=2000), "limits"), (dict(P=0), "P must"),
     (dict(P=65537), "P must"), (dict(B=8192, Hkv=1024), "2^23"), (dict(reserved=1), "reserved"), (dict(path=None), "null"), (dict(path=TAB + 1), "aligned"),
-    (dict(len_out=None), "null"), (dict(len_out=LEN + 8), "overlaps len"), (dict(cache={"k": None}), "null"),
+    (dict(len_out=None), "null"), (dict(len_out=LEN + 8), "overlaps len"), (dict(path=LEN2 + 16), "overlaps path"), (dict(len_out=MASK), "overlaps path or n_path"),
+    (dict(cache={"k": None}), "null"),
 ])
 def test_commit_refuses(kw, word):
     kw = dict(kw)
