@@ -300,8 +300,9 @@ def against_dense(ctx, c, q, dtype, n_rows, parents, clean=None, but=None):
     return out, lse
 
 
+@pytest.mark.parametrize("kind", ["chain", "tree"])
 @pytest.mark.parametrize("dtype,B,T,Hq,Hkv,d,slots,page", LONG)
-def test_every_cut_matches_the_formula(ctx, dtype, B, T, Hq, Hkv, d, slots, page):
+def test_every_cut_matches_the_formula(ctx, dtype, B, T, Hq, Hkv, d, slots, page, kind):
     seed = B * T + slots
     r = np.random.default_rng(seed)
     n_rows = [T] + r.integers(1, T + 1, B - 1).tolist()
@@ -309,7 +310,7 @@ def test_every_cut_matches_the_formula(ctx, dtype, B, T, Hq, Hkv, d, slots, page
     lens = np.array(n_rows)[:, None] + np.where(r.random((B, Hkv)) < 0.5, most, r.integers(0, most + 1, (B, Hkv)))
     c = Caches(dtype, lens.tolist(), slots, d, page, seed).dev()
     q = torch.randn(B, T, Hq, d, generator=torch.Generator().manual_seed(seed)).to(dtype).to(DEV)
-    parents = [tree_of(T, seed + b) for b in range(B)] if seed % 2 else None
+    parents = [tree_of(T, seed + b) for b in range(B)] if kind == "tree" else None
     against_dense(ctx, c, q, dtype, n_rows, parents)
 
 
@@ -605,6 +606,40 @@ def test_drafting_and_keeping_a_path_is_decoding_it_token_by_token(ctx, dtype, p
                     f1, f2 = ((y.reshape(-1, d) if y.shape[-1] == d and y.dim() == (3 if page else 4) else y.reshape(-1)) for y in (c1, c2))
                     assert torch.equal(f1[rows], f2[rows])
         base += 3
+
+
+def test_two_graphs_share_a_workspace_and_follow_the_lengths(ctx):
+    """Two captured calls, one of runs dealt out by the lengths and one of runs by the slots, replayed in turn while the lengths and
+    the queries change, against eager calls."""
+    long, short = (Caches(BF, [[4096] * 8] * 16, 4096, 128, 0, 73).dev(), Caches(BF, [[5000] * 2], 5000, 128, 0, 74).dev())
+    q = [torch.zeros(16, 32, 32, 128, dtype=BF, device=DEV), torch.zeros(1, 3, 8, 128, dtype=BF, device=DEV)]
+    out = [torch.zeros_like(x) for x in q]
+    ctx.reserve(1 << 27)
+
+    def call(i, o, **kw):
+        c = (long, short)[i]
+        return ctx.tree_attn(q[i], c.k, c.v, c.len, out=o, **kw)[0]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call(0, out[0], reserve=False)
+        call(1, out[1], reserve=False)
+    torch.cuda.synchronize()
+    graphs = [torch.cuda.CUDAGraph() for _ in q]
+    for i, g in enumerate(graphs):
+        with torch.cuda.graph(g):
+            call(i, out[i], reserve=False)
+    r = torch.Generator().manual_seed(75)
+    for rnd in range(4):
+        for x in q:
+            x.copy_(torch.randn(x.shape, generator=r).to(BF))
+        long.len.copy_((torch.rand(long.len.shape, generator=r) ** (1 + 2 * rnd) * 4064).to(torch.int32) + 32)
+        short.len.copy_(torch.tensor([[5000 - 700 * rnd, 3 + rnd]], dtype=torch.int32))
+        for g in (graphs if rnd % 2 else graphs[::-1]):
+            g.replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert torch.equal(out[i], call(i, torch.empty_like(out[i]))), (rnd, i)
+        torch.cuda.synchronize()
 
 
 def test_another_stream_and_two_calls_in_a_row(ctx):

@@ -94,6 +94,11 @@ def test_tree_attention_refuses(kw, word):
     assert st == 1 and word in why, (st, why)
 
 
+def test_tree_attention_names_the_workspace_it_lacks():
+    st, why = _tree(desc={"Lmax": 8192}, cache={"Lmax": 8192})      # (few rows over long lists: runs, whose sums lie there)
+    assert st == 3 and "workspace" in why, (st, why)
+
+
 @pytest.mark.parametrize("kw,word", [
     (dict(hd=96), "head dimension"), (dict(dtype=2), "dtype"), (dict(B=0), "positive"), (dict(Hkv=2000), "limits"), (dict(P=0), "P must"),
     (dict(P=65537), "P must"), (dict(B=8192, Hkv=1024), "2^23"), (dict(reserved=1), "reserved"), (dict(path=None), "null"), (dict(path=TAB + 1), "aligned"),
