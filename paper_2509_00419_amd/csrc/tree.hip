@@ -299,9 +299,9 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
 #pragma unroll
                         for (int y = 0; y < ND; y += 4)
                             asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1\n\tglobal_load_lds_dwordx4 %3, %1 offset:1024\n\t"
-                                         "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:3072"
+                                         "global_load_lds_dwordx4 %4, %1 offset:2048\n\tglobal_load_lds_dwordx4 %5, %1 offset:%6"
                                          ::"v"(turned(y)), "s"(src + 1024 * y), "s"(__builtin_amdgcn_readfirstlane(dst + 1024u * y)), "v"(turned(y + 1)),
-                                           "v"(turned(y + 2)), "v"(turned(y + 3)) : "memory", "m0");
+                                           "v"(turned(y + 2)), "v"(turned(y + 3)), "n"(3 * 1024) : "memory", "m0");
                     }
                 }
             } else {                                // rows past the last entry repeat it (and are masked)
