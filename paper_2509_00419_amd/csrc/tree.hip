@@ -509,9 +509,9 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
         }
         // A value that is no number must not reach the rows that do not see it -- their weight for it is 0, and 0 times it is
         // not: in a tile that has any they are left out of the product, and added to the rows that do see them.  (A repeat of
-        // the last entry is not seen either.)
+        // the last entry is not seen either, nor need a row see itself where there is a mask.)
         bool odd = false;
-        if (in != ~0u || (d < 32 && n > 1)) {
+        if (in != ~0u || (d < 32 && (n > 1 || a.mask))) {
             // the largest exponent of all (in bf16 of both halves of a word)
             typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
             u16x2 top2 = {0, 0};
