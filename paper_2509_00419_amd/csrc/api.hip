@@ -714,7 +714,7 @@ lvlm_status lvlm_kv_append(lvlm_ctx *ctx, void *stream, const lvlm_append_desc *
     if (const char *why = check_lengths(len, len_out, d->B, d->Hkv)) return fail(ctx, LVLM_ERR_INVALID_ARG, "kv_append: %s", why);
     const size_t heads = (size_t)d->B * d->Hkv * 4;
     const size_t axes = d->rot_dim > 0 ? (size_t)d->n_axes : 1;       // (without turning axis 0 names the entries' positions)
-    if (overlap(src->n_new, span(d->B, 1, d->Hkv, 1, d->n_stride_b, 0, d->n_stride_h, 4), len_out, heads) ||
+    if ((src->n_new && overlap(src->n_new, span(d->B, 1, d->Hkv, 1, d->n_stride_b, 0, d->n_stride_h, 4), len_out, heads)) ||
         (src->pos && overlap(src->pos, axes * d->B * d->T * 4, len_out, heads)))
         return fail(ctx, LVLM_ERR_INVALID_ARG, "kv_append: len_out overlaps n_new or pos");
     if (d->T == 0 && len == len_out) return LVLM_OK;

@@ -36,3 +36,10 @@ def test_axes_are_not_read_where_nothing_turns(n_axes):
     st, why = abi._append(desc=desc, src={**PLAIN, "pos": LEN2 - 36})
     assert st == 1 and "len_out overlaps n_new or pos" in why
     assert passes(abi._append(desc=desc, src={**PLAIN, "pos": LEN2 - 40}))      # [2, 5] positions end where the lengths begin
+
+
+def test_strides_of_counts_that_are_not_given_make_no_range():
+    assert passes(abi._append(desc={"n_stride_b": 1 << 36, "n_stride_h": 1 << 36}))
+    st, why = abi._append(desc={"n_stride_b": 1}, src={"n_new": LEN2 - 4})
+    assert st == 1 and "len_out overlaps n_new" in why
+    assert passes(abi._append(desc={"n_stride_b": 1}, src={"n_new": LEN2 - 8}))
