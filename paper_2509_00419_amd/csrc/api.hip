@@ -226,7 +226,7 @@ const char *check_append(const lvlm_append_desc *d, const lvlm_append_src *s, co
     if (s->q && d->rot_dim == 0) return "q is only passed to be turned (rot_dim > 0)";
     if (s->q && s->n_new && d->n_stride_h != 0) return "q needs counts per sequence (n_stride_h 0)";
     if (d->rot_dim > 0) {
-        if (!s->pos || !s->inv_freq) return "pos and inv_freq are needed to turn";
+        if ((d->T > 0 && !s->pos) || !s->inv_freq) return "pos and inv_freq are needed to turn";
         if (d->n_axes < 1 || d->n_axes > 3) return "n_axes must be 1, 2 or 3";
         long long sum = 0;
         for (int i = 0; i < d->n_axes; ++i) {
@@ -247,8 +247,9 @@ const char *check_append(const lvlm_append_desc *d, const lvlm_append_src *s, co
     if ((why = check_rows(d->B, T, d->Hkv, d->hd, d->k_stride_b, d->k_stride_t, d->k_stride_h, vec, false))) return why;
     if ((why = check_rows(d->B, T, d->Hkv, d->hd, d->v_stride_b, d->v_stride_t, d->v_stride_h, vec, false))) return why;
     const size_t cb = cache_bytes(*c, d->B, d->Hkv, (size_t)d->hd * eb);
-    const size_t kb = span(d->B, T, d->Hkv, d->hd, d->k_stride_b, d->k_stride_t, d->k_stride_h, eb);
-    const size_t vb = span(d->B, T, d->Hkv, d->hd, d->v_stride_b, d->v_stride_t, d->v_stride_h, eb);
+    // (without new rows there is nothing of them to overlap)
+    const size_t kb = d->T > 0 ? span(d->B, T, d->Hkv, d->hd, d->k_stride_b, d->k_stride_t, d->k_stride_h, eb) : 0;
+    const size_t vb = d->T > 0 ? span(d->B, T, d->Hkv, d->hd, d->v_stride_b, d->v_stride_t, d->v_stride_h, eb) : 0;
     if (overlap(s->k, kb, c->k, cb) || overlap(s->k, kb, c->v, cb) || overlap(s->v, vb, c->k, cb) || overlap(s->v, vb, c->v, cb))
         return "new rows overlap the cache";
     if (overlap(c->k, cb, c->v, cb)) return "the cache's keys and values overlap";
@@ -259,8 +260,8 @@ const char *check_append(const lvlm_append_desc *d, const lvlm_append_src *s, co
     if (s->q) {
         if ((why = check_rows(d->B, T, d->Hq, d->hd, d->q_stride_b, d->q_stride_t, d->q_stride_h, vec, false))) return why;
         if ((why = check_rows(d->B, T, d->Hq, d->hd, d->qo_stride_b, d->qo_stride_t, d->qo_stride_h, vec, true))) return why;
-        const size_t qb = span(d->B, T, d->Hq, d->hd, d->q_stride_b, d->q_stride_t, d->q_stride_h, eb);
-        const size_t ob = span(d->B, T, d->Hq, d->hd, d->qo_stride_b, d->qo_stride_t, d->qo_stride_h, eb);
+        const size_t qb = d->T > 0 ? span(d->B, T, d->Hq, d->hd, d->q_stride_b, d->q_stride_t, d->q_stride_h, eb) : 0;
+        const size_t ob = d->T > 0 ? span(d->B, T, d->Hq, d->hd, d->qo_stride_b, d->qo_stride_t, d->qo_stride_h, eb) : 0;
         const bool same = s->q == s->q_out && d->q_stride_b == d->qo_stride_b && d->q_stride_t == d->qo_stride_t &&
                           d->q_stride_h == d->qo_stride_h;
         if (!same && overlap(s->q, qb, s->q_out, ob)) return "q_out overlaps q (it may only be q itself)";

@@ -4,7 +4,7 @@ import pytest
 
 import paper_2509_00419_amd as lv
 import test_tree_abi as abi
-from test_tree_abi import LEN, LEN2
+from test_tree_abi import K, LEN, LEN2, V
 
 NOWHERE = 99        # a device that no machine has
 
@@ -43,3 +43,15 @@ def test_strides_of_counts_that_are_not_given_make_no_range():
     st, why = abi._append(desc={"n_stride_b": 1}, src={"n_new": LEN2 - 4})
     assert st == 1 and "len_out overlaps n_new" in why
     assert passes(abi._append(desc={"n_stride_b": 1}, src={"n_new": LEN2 - 8}))
+
+
+def test_no_new_rows_read_nothing():
+    """T = 0: positions and rows of such a call have no elements, and torch gives arrays without elements no address."""
+    nothing = {"k": None, "v": None, "q": None, "q_out": None, "pos": None}
+    assert abi._append(desc={"T": 0}, src=nothing, length=(LEN, LEN)) == (0, "")
+    assert passes(abi._append(desc={"T": 0}, src=nothing))
+    assert passes(abi._append(desc={"T": 0}, src={"k": K + 4096, "v": V, "q": K, "q_out": V}))
+    assert passes(abi._append(desc={"T": 0}, src={"pos": LEN2}))
+    for missing in ("pos", "inv_freq"):
+        st, why = abi._append(src={missing: None})
+        assert st == 1 and "pos and inv_freq" in why
