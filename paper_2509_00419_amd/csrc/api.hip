@@ -325,11 +325,13 @@ lvlm_status after_launch(lvlm_ctx *ctx, hipError_t e) {
     return LVLM_OK;
 }
 
-lvlm_status bind_device(lvlm_ctx *ctx) {
-    const hipError_t e = hipSetDevice(ctx->device);
-    if (e != hipSuccess) return fail(ctx, LVLM_ERR_HIP, "hipSetDevice(%d): %s", ctx->device, hipGetErrorString(e));
-    return LVLM_OK;
+// The error is this call's: HIP keeps it, and the next launch would report it as its own.
+lvlm_status device_status(lvlm_ctx *ctx, hipError_t e) {
+    if (e == hipSuccess) return LVLM_OK;
+    (void)hipGetLastError();
+    return fail(ctx, LVLM_ERR_HIP, "hipSetDevice(%d): %s", ctx->device, hipGetErrorString(e));
 }
+lvlm_status bind_device(lvlm_ctx *ctx) { return device_status(ctx, hipSetDevice(ctx->device)); }
 
 // The context's device for the length of a call; the caller's current one is put back.
 struct DeviceScope {
@@ -342,9 +344,7 @@ struct DeviceScope {
     ~DeviceScope() {
         if (before >= 0 && before != device) (void)hipSetDevice(before);
     }
-    lvlm_status status(lvlm_ctx *ctx) const {
-        return err == hipSuccess ? LVLM_OK : fail(ctx, LVLM_ERR_HIP, "hipSetDevice(%d): %s", device, hipGetErrorString(err));
-    }
+    lvlm_status status(lvlm_ctx *ctx) const { return device_status(ctx, err); }
 };
 
 }  // namespace
