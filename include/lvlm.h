@@ -501,7 +501,7 @@ typedef struct {          /* HOST struct of device pointers                     
  * len_out[b][g] = len[b][g] + n.  On the way keys and queries are turned by their position: pair c of the rot_dim / 2
  * pairs, of axis a by the sections, turns by the angle pos[a][b][t] * inv_freq[c],
  *   x_i' = x_i cos - x_j sin,  x_j' = x_j cos + x_i sin,
- * angles reduced in 64 bits (exact at any 32-bit position), products in fp32, one rounding to the dtype; channels from
+ * angles reduced in 64-bit words (to 2^-25 of a turn at any 32-bit position), products in fp32, one rounding to the dtype; channels from
  * rot_dim on, and values, are copied.  q_out[b][t] for t < n; rows from n on (all T have to be readable) are not written.
  * A head whose entries do not all fit (len + n > Lmax, or a negative len) takes none of them and keeps its length: a caller
  * that cannot rule this out compares the lengths.  Without turning and with counts per head the call packs compressed lists,

@@ -2,6 +2,7 @@
 // accepted ones of them moved together behind the committed entries.
 #include "mma.h"
 #include "pages.h"
+#include "turns.h"
 
 #include <algorithm>
 
@@ -95,8 +96,7 @@ __device__ __forceinline__ bool fits(const AppendArgs &a, int len, int n) { retu
 
 // A thread owns 16 channels (eight pairs) of one token: it works the eight angles out once and goes through some of the
 // token's heads with them.  A row of keys or queries passes as 16-byte words, those of eight (hd 128) or four (hd 64) threads
-// next to each other.  Angles: position times frequency in 64 bits, a 31-bit by a 24-bit number and so all but exact, in
-// turns; what is left of the whole turns goes to fp32, where a turn is off by 2^-25 at most, whatever the position.
+// next to each other.  Angles are worked out in 64 bits, in turns; what is left of the whole turns goes to fp32 (turns.h).
 //
 // What bounds it: a long call the memory (a row in, a row out), a short one its trips to memory.  A head's rows, its length
 // and what is known of its entries are asked for a head ahead, the first one's before the angles, so a short call waits for
@@ -159,8 +159,7 @@ __global__ __launch_bounds__(256) void kv_append_kernel(AppendArgs a) {
 #pragma unroll
         for (int c = 0; c < 8; ++c) {
             const int pair = 8 * s + c, p = pair < a.end0 ? p0 : pair < a.end1 ? p1 : p2;
-            const double rev = (double)p * (double)freq[c] * 0.15915494309189533577;    // 1 / (2 pi)
-            sincospif(2.f * (float)(rev - rint(rev)), &sn[c], &cs[c]);
+            sincospif(2.f * part_of_turn(p, freq[c]), &sn[c], &cs[c]);
         }
     }
     for (int i = 0; i < a.per_thread; ++i) {

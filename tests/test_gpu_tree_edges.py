@@ -38,3 +38,36 @@ def test_a_refused_device_is_not_reported_by_the_next_call(ctx):
         s = torch.cuda.current_stream().cuda_stream
         assert bd.lib.lvlm_kv_append(context._h, s, C.byref(d), C.byref(bd.AppendSrc()), C.byref(cache), c.len.data_ptr(), out.data_ptr()) == status
     assert torch.equal(out, c.len)
+
+
+@pytest.mark.parametrize("adjacent", [False, True])
+def test_far_positions_turn_as_exactly_as_near_ones(ctx, adjacent):
+    """Unit keys and queries become the cosine and sine of their angles: 2^-25 of a turn off at most (2 pi 2^-25), by which either changes as
+    much at most, and 4 ulp of a number up to 1 (2^-22) for the function itself; the products are with 1 and 0.  Frequencies of hundreds,
+    positions near the last there are: 2^38 turns, of which one 64-bit word keeps 2^-15."""
+    import math
+    from fractions import Fraction
+    two_pi = 2 * Fraction("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534211706798214808651")
+    T, d = 37, 64
+    g = torch.Generator().manual_seed(5)
+    freq = torch.cat([torch.rand(28, generator=g) * 500 + 500, torch.tensor([1.0, 0.5, 1e-6, 0.0])])
+    pos = torch.randint(2 ** 30, 2 ** 31 - 1, (1, T), generator=g, dtype=torch.int64)
+    pos[0, ::3] *= -1
+    pos[0, :2] = torch.tensor([2 ** 31 - 1, -2 ** 31])
+    want = torch.empty(T, 32, 2, dtype=torch.float64)
+    for t in range(T):
+        for c in range(32):
+            turns = int(pos[0, t]) * Fraction(float(freq[c])) / two_pi
+            part = 2 * math.pi * float(turns - round(turns))
+            want[t, c, 0], want[t, c, 1] = math.cos(part), math.sin(part)
+    one = torch.zeros(1, T, 1, d)
+    one[..., 0::2] = 1.0
+    if not adjacent:
+        one = torch.cat([torch.ones(1, T, 1, 32), torch.zeros(1, T, 1, 32)], dim=-1)
+    one = one.to(DEV)
+    c = Caches(torch.float32, [[0]], 48, d).dev()
+    _, q = ctx.kv_append(one, one, c.k, c.v, c.len, pos=pos.to(torch.int32).to(DEV), inv_freq=freq.to(DEV), adjacent=adjacent, q=one)
+    for x in (c.k[0, 0, :T], q[0, :, 0]):
+        x = x.double().cpu()
+        x = x.view(T, 32, 2) if adjacent else x.view(T, 2, 32).transpose(1, 2)
+        assert float((x - want).abs().max()) <= 2 * math.pi * 2.0 ** -25 + 2.0 ** -22
