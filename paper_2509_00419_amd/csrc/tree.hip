@@ -508,8 +508,8 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
             l[x] += weigh(s[x], m[x] == -INFINITY ? 0.f : m[x]);
         }
         // A value that is no number must not reach the rows that do not see it -- their weight for it is 0, and 0 times it is
-        // not: in a tile that has any they are left out of the product, and added to the rows that do see them.  (A repeat of
-        // the last entry is not seen either, nor need a row see itself where there is a mask.)
+        // not: in a tile that has any they are left out of the product, and added to the rows that do see them, whatever their
+        // weight there.  (A repeat of the last entry is not seen either, nor need a row see itself where there is a mask.)
         bool odd = false;
         if (in != ~0u || (d < 32 && (n > 1 || a.mask))) {
             // the largest exponent of all (in bf16 of both halves of a word)
@@ -557,7 +557,7 @@ __global__ __launch_bounds__(256, (TreeShape<DT, HD, RB, KW>::PER_CU)) void tree
                             }
 #pragma unroll
                             for (int c = 0; c < 4; ++c)
-                                if (!(p == 0.f) && (v[c] & 0x7f800000u) == 0x7f800000u)
+                                if ((sees[x] >> key & 1u) && (v[c] & 0x7f800000u) == 0x7f800000u)
                                     o[x][cb][4 * r4 + c] = fmaf(p, __uint_as_float(v[c]), o[x][cb][4 * r4 + c]);
                         }
                 }

@@ -51,3 +51,23 @@ def test_a_row_that_does_not_see_itself_stays_clear_of_its_own_value(ctx, dtype,
         assert bool(((lse[:, :, 0].double() - ref_lse[:, :, 0]).abs() <= e + (length + 4) * U + 4 * U * ref_lse[:, :, 0].abs()).all())
         clean = out if clean is None else clean
         assert torch.equal(out, clean), (bad_k, bad_v)
+
+
+@pytest.mark.parametrize("L,at", [(40, 35), (40, 3), (300, 290), (64, 60)])
+@pytest.mark.parametrize("dtype,T,G", [(BF, 1, 8), (BF, 5, 2), (BF, 1, 300), (FP, 1, 8), (FP, 5, 4), (FP, 1, 2)])
+def test_what_a_row_sees_is_not_hidden_by_a_weight_of_zero(ctx, dtype, T, G, L, at):
+    """An entry whose weight is below what fp32 holds: times an infinity that is no finite number, in any tile."""
+    d = 64
+    c = Caches(dtype, [[L + T]], 320, d, 0, L).dev()
+    c.k[0, 0, at] = -8.0
+    q = torch.full((1, T, G, d), 4.0, device=DEV).to(dtype)                  # (logit -256; the others' are a hundredth of that)
+    c.k[0, 0, :at].mul_(0.01)
+    c.k[0, 0, at + 1:].mul_(0.01)
+    clean, clean_lse = ctx.tree_attn(q, c.k, c.v, c.len, want_lse=True)
+    c.v[0, 0, at, 3], c.v[0, 0, at, 40] = float("inf"), float("nan")
+    out, lse = ctx.tree_attn(q, c.k, c.v, c.len, want_lse=True)
+    odd = torch.tensor([3, 40], device=DEV)
+    assert not bool(torch.isfinite(out[..., odd].float()).any())
+    keep = torch.ones(d, dtype=torch.bool, device=DEV)
+    keep[odd] = False
+    assert torch.equal(out[..., keep], clean[..., keep]) and torch.equal(lse, clean_lse)
