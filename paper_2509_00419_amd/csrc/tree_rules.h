@@ -30,6 +30,7 @@ struct TreeForm {
     float busy;             // us of a compute unit for a tile of one row block, on a chip that has all it can do
     int rows() const { return rb == 0 ? kFewRows : 32 * rb * (4 / kw); }     // (rb 0: fp32, few rows on the vector ALUs; a workgroup takes 0.6 us more for each,
                                                                         // a tile as long again)
+    int threads() const { return rb == 0 ? 512 : 256; }
 };
 constexpr int kTreeForms = 4;
 inline const TreeForm *tree_forms(const lvlm_tree_desc &d, int &n) {
@@ -65,7 +66,8 @@ inline TreeWs tree_cut(const lvlm_tree_desc &d) {
         for (int wanted : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
             if (wanted > steps) break;
             const long long run = (steps + wanted - 1) / wanted, split = (steps + run - 1) / run;
-            if (pairs * blocks * split >= (1ll << 23) || (split > 1 && pairs > 65535)) break;     // a launch's most (the fold's: by pairs)
+            // a launch's most, half of 2^32 threads (the fold's: by pairs)
+            if (pairs * blocks * split * f.threads() >= (1ll << 31) || (split > 1 && pairs > 65535)) break;
             const double per_unit = (double)(pairs * blocks * split) / kUnits, whole = (double)((pairs * blocks * split + kUnits - 1) / kUnits);
             const double rounds = per_unit > 8 ? per_unit : whole;
             double t = (begin + tile * (double)(run * f.tps)) * (rounds <= 1 ? 1.0 : rounds * f.shared);
