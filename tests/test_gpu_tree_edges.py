@@ -71,3 +71,23 @@ def test_far_positions_turn_as_exactly_as_near_ones(ctx, adjacent):
         x = x.double().cpu()
         x = x.view(T, 32, 2) if adjacent else x.view(T, 2, 32).transpose(1, 2)
         assert float((x - want).abs().max()) <= 2 * math.pi * 2.0 ** -25 + 2.0 ** -22
+
+
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+def test_as_many_lists_as_a_call_may_have(ctx, dtype):
+    """2^23 - 2 lists of one entry: a row's result is its value.  fp32: the probability is not 1 where the scaled logit was rounded, and is divided by
+    itself: three roundings, and that of the product, of 2^-24 each."""
+    B, H, d = 12282, 683, 64
+    g = torch.Generator(device=DEV).manual_seed(3)
+    k, v, q = (torch.randn(B, H, 1, d, generator=g, device=DEV).to(dtype) for _ in range(3))
+    length = torch.ones(B, H, dtype=torch.int32, device=DEV)
+    out, lse = ctx.tree_attn(q.view(B, 1, H, d), k, v, length, want_lse=True)
+    v = v.view(B, 1, H, d)
+    if dtype == BF:
+        assert torch.equal(out, v)
+    else:
+        assert bool(((out - v).abs() <= 4 * 2.0 ** -24 * v.abs()).all())
+    for b, h in ((0, 0), (B // 2, 5), (B - 1, H - 1)):
+        x = q[b, h, 0].double() * k[b, h, 0].double() * d ** -0.5
+        off = abs(float(lse[b, h, 0]) - float(x.sum()))
+        assert off <= 2.0 ** -24 * ((d + 4) * float(x.abs().sum()) + 5 + 4 * abs(float(x.sum())))       # (as in test_gpu_tree.py)
