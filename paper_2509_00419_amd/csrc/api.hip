@@ -186,6 +186,35 @@ bool overlap(const void *p, size_t n, const void *q, size_t m) {
 size_t span(int B, int T, int H, int hd, long long sb, long long st, long long sh, int eb) {
     return (size_t)((B - 1) * sb + (T - 1) * st + (H - 1) * sh + hd) * eb;
 }
+// Rows x[b][t][h][0..hd) of heads and strides of their own.
+struct Rows {
+    const void *p;
+    int H;
+    long long sb, st, sh;
+};
+// Do x and y share elements?  Where their ranges do, they may still be slices of one buffer that go through it in the same steps: all heads'
+// rows of a token in a part of the step of their own, or all tokens' of a sequence.  (Other ways past each other are taken for an overlap.)
+bool rows_overlap(const Rows &x, const Rows &y, int B, int T, int hd, int eb) {
+    if (!overlap(x.p, span(B, T, x.H, hd, x.sb, x.st, x.sh, eb), y.p, span(B, T, y.H, hd, y.sb, y.st, y.sh, eb))) return false;
+    if (B > 1 && x.sb != y.sb) return true;
+    const auto apart = [&](long long step, size_t nx, size_t ny) {      // y from x, modulo the step, behind x's part and before the next x
+        if (step <= 0) return false;
+        step *= eb;
+        const long long by = (long long)(reinterpret_cast<uintptr_t>(y.p) - reinterpret_cast<uintptr_t>(x.p)), r = (by % step + step) % step;
+        return r >= (long long)nx && step - r >= (long long)ny;
+    };
+    if (B > 1 && apart(x.sb, span(1, T, x.H, hd, 0, x.st, x.sh, eb), span(1, T, y.H, hd, 0, y.st, y.sh, eb))) return false;
+    if (T > 1 && x.st == y.st) {
+        long long step = x.st, rest = B > 1 ? x.sb : 0;
+        while (rest != 0) {                         // what both steps are multiples of
+            const long long r = step % rest;
+            step = rest;
+            rest = r;
+        }
+        if (apart(step, span(1, 1, x.H, hd, 0, 0, x.sh, eb), span(1, 1, y.H, hd, 0, 0, y.sh, eb))) return false;
+    }
+    return true;
+}
 constexpr long long kMaxStride = 1ll << 36;     // times any size, and the element size, within 63 bits
 // Strides of rows x[b][t][h]: whole vectors; no two rows of an output share elements.
 const char *check_rows(int B, int T, int H, int hd, long long sb, long long st, long long sh, int vec, bool written) {
@@ -264,7 +293,10 @@ const char *check_append(const lvlm_append_desc *d, const lvlm_append_src *s, co
         const size_t ob = d->T > 0 ? span(d->B, T, d->Hq, d->hd, d->qo_stride_b, d->qo_stride_t, d->qo_stride_h, eb) : 0;
         const bool same = s->q == s->q_out && d->q_stride_b == d->qo_stride_b && d->q_stride_t == d->qo_stride_t &&
                           d->q_stride_h == d->qo_stride_h;
-        if (!same && overlap(s->q, qb, s->q_out, ob)) return "q_out overlaps q (it may only be q itself)";
+        if (!same && d->T > 0 &&
+            rows_overlap({s->q, d->Hq, d->q_stride_b, d->q_stride_t, d->q_stride_h},
+                         {s->q_out, d->Hq, d->qo_stride_b, d->qo_stride_t, d->qo_stride_h}, d->B, d->T, d->hd, eb))
+            return "q_out overlaps q (it may only be q itself)";
         if (overlap(s->q, qb, c->k, cb) || overlap(s->q, qb, c->v, cb) || overlap(s->q_out, ob, c->k, cb) ||
             overlap(s->q_out, ob, c->v, cb))
             return "q or q_out overlaps the cache";
@@ -738,7 +770,8 @@ lvlm_status lvlm_tree_attn(lvlm_ctx *ctx, void *stream, const lvlm_tree_desc *d,
     const size_t qb = span(d->B, d->T, d->Hq, d->hd, d->q_stride_b, d->q_stride_t, d->q_stride_h, eb);
     const size_t ob = span(d->B, d->T, d->Hq, d->hd, d->o_stride_b, d->o_stride_t, d->o_stride_h, eb);
     const size_t cb = cache_bytes(*cache, d->B, d->Hkv, (size_t)d->hd * eb);
-    if (overlap(q, qb, out, ob) || overlap(cache->k, cb, out, ob) || overlap(cache->v, cb, out, ob))
+    if (rows_overlap({q, d->Hq, d->q_stride_b, d->q_stride_t, d->q_stride_h}, {out, d->Hq, d->o_stride_b, d->o_stride_t, d->o_stride_h}, d->B,
+                     d->T, d->hd, eb) || overlap(cache->k, cb, out, ob) || overlap(cache->v, cb, out, ob))
         return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: out overlaps q or the cache");
     const size_t lb = (size_t)d->B * d->Hq * d->T * 4;
     if (row_lse && (overlap(row_lse, lb, q, qb) || overlap(row_lse, lb, out, ob) || overlap(row_lse, lb, cache->k, cb) ||

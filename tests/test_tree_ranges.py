@@ -4,7 +4,7 @@ import pytest
 
 import paper_2509_00419_amd as lv
 import test_tree_abi as abi
-from test_tree_abi import K, LEN, LEN2, V
+from test_tree_abi import K, LEN, LEN2, Q, V
 
 NOWHERE = 99        # a device that no machine has
 
@@ -55,3 +55,28 @@ def test_no_new_rows_read_nothing():
     for missing in ("pos", "inv_freq"):
         st, why = abi._append(src={missing: None})
         assert st == 1 and "pos and inv_freq" in why
+
+
+def refused(result):
+    st, why = result
+    return st == 1 and "overlap" in why
+
+
+def test_slices_of_one_buffer_do_not_overlap():
+    """Rows of 1024 elements for q and 512 each for k and v, one after the other in a buffer: the ranges reach into each other, the rows do not."""
+    row = 1024 + 512 + 512
+    strides = {f"{x}_stride_{a}": n for x in ("q", "k", "v") for a, n in (("b", 5 * row), ("t", row))}
+    qo = {"qo_stride_b": 5 * row, "qo_stride_t": row}
+    src = {"q": Q, "k": Q + 2 * 1024, "v": Q + 2 * 1536}
+    assert passes(abi._append(desc={**strides, **qo}, src={**src, "q_out": Q}))
+    # q turned into a slice of its own behind v's
+    wide = {f"{x}_stride_{a}": n for x in ("q", "qo", "k", "v") for a, n in (("b", 5 * (row + 1024)), ("t", row + 1024))}
+    assert passes(abi._append(desc=wide, src={**src, "q_out": Q + 2 * row}))
+    assert refused(abi._append(desc=wide, src={**src, "q_out": Q + 2 * (row + 8)}))                   # ... into the next row's q
+    # heads before tokens, [B, heads, T, d]: the sequences' steps are what is left
+    heads = {f"{x}_stride_{a}": n for x in ("q", "qo") for a, n in (("b", 16 * 5 * 128), ("t", 128), ("h", 5 * 128))}
+    assert passes(abi._append(desc=heads, src={"q_out": Q + 2 * 8 * 5 * 128}))
+    assert refused(abi._append(desc=heads, src={"q_out": Q + 2 * 7 * 5 * 128}))
+    # the same for attention
+    both = {f"{x}_stride_{a}": n for x in ("q", "o") for a, n in (("b", 5 * row), ("t", row))}
+    assert passes(abi._tree(desc=both, out=Q + 2 * 1024)) and refused(abi._tree(desc=both, out=Q + 2 * 1016))
