@@ -506,7 +506,8 @@ typedef struct {          /* HOST struct of device pointers                     
  * A head whose entries do not all fit (len + n > Lmax, or a negative len) takes none of them and keeps its length: a caller
  * that cannot rule this out compares the lengths.  Without turning and with counts per head the call packs compressed lists,
  * with their score, kind and orig_pos, into pages.  len_out may be len itself.  q needs counts per sequence (n_stride_h 0) and
- * rot_dim > 0.  New rows (and their score, kind and orig_pos) must not overlap the cache, nor len_out n_new or pos.  No workspace. */
+ * rot_dim > 0.  What the call writes (the cache's arrays, q_out, len_out) must not overlap anything else that it is given, but as said
+ * above; slices of one buffer's rows do not overlap.  Places that are written belong to one head alone.  No workspace. */
 LVLM_API lvlm_status lvlm_kv_append(lvlm_ctx *ctx, void *stream, const lvlm_append_desc *d, const lvlm_append_src *src,
                                     const lvlm_cache *cache, const int32_t *len, int32_t *len_out);
 
@@ -533,7 +534,7 @@ typedef struct {
  * writes zeros and -inf; rows from n on are left as they were.  What a row does not see adds nothing to it, whatever it holds
  * (NaN and infinities included).  T = 1 is plain decoding from such a cache.  Entries at or beyond len_bound are not read.
  * q is turned already (lvlm_kv_append).  row_lse [B, Hq, T] fp32 may be NULL.  out and row_lse must not overlap
- * each other, q or the cache.
+ * each other or anything that the call reads (q's and out's rows may be slices of one buffer's).
  * The importance of the entries is left as it is.  Workspace: LVLM_OP_TREE_ATTN. */
 LVLM_API lvlm_status lvlm_tree_attn(lvlm_ctx *ctx, void *stream, const lvlm_tree_desc *d, const void *q,
                                     const lvlm_cache *cache, const int32_t *len, const int32_t *n_rows,
@@ -556,7 +557,8 @@ typedef struct {
  * len + path[b][i] moves to slot len + i, and len_out = len + n_path.  A path that stops ascending, turns negative or leaves
  * the Lmax slots ends before that place; a head with a negative len, or none of whose slots are left, keeps its length.
  * An entry that would move from or to a page outside the pool is left.
- * path [B, P] i32, n_path [B] i32 (device).  len_out may be len itself, but not overlap path or n_path.
+ * path [B, P] i32, n_path [B] i32 (device).  len_out may be len itself; else neither it nor the cache's arrays may overlap each other or
+ * anything that the call reads.
  * No workspace. */
 LVLM_API lvlm_status lvlm_tree_commit(lvlm_ctx *ctx, void *stream, const lvlm_commit_desc *d, const lvlm_cache *cache,
                                       const int32_t *len, const int32_t *path, const int32_t *n_path, int32_t *len_out);

@@ -186,6 +186,31 @@ bool overlap(const void *p, size_t n, const void *q, size_t m) {
 size_t span(int B, int T, int H, int hd, long long sb, long long st, long long sh, int eb) {
     return (size_t)((B - 1) * sb + (T - 1) * st + (H - 1) * sh + hd) * eb;
 }
+// Outputs against each other and against what the call reads, which other workgroups may not have read yet.
+struct Range {
+    const void *p;
+    size_t n;
+};
+const char *check_apart(const Range *out, int n_out, const Range *in, int n_in) {
+    for (int i = 0; i < n_out; ++i) {
+        for (int j = 0; j < i; ++j)
+            if (overlap(out[i].p, out[i].p ? out[i].n : 0, out[j].p, out[j].p ? out[j].n : 0)) return "two outputs overlap";
+        for (int j = 0; j < n_in; ++j)
+            if (overlap(out[i].p, out[i].p ? out[i].n : 0, in[j].p, in[j].p ? in[j].n : 0)) return "an output overlaps what the call reads";
+    }
+    return nullptr;
+}
+constexpr int kCacheRanges = 5;
+void cache_ranges(const lvlm_cache &c, int B, int Hkv, size_t row, Range *to) {
+    const size_t slots = cache_bytes(c, B, Hkv, 1);
+    to[0] = {c.k, slots * row};
+    to[1] = {c.v, slots * row};
+    to[2] = {c.score, slots * 4};
+    to[3] = {c.kind, slots};
+    to[4] = {c.orig_pos, slots * 4};
+}
+Range page_range(const lvlm_cache &c, int B, int Hkv) { return {c.pages, c.pages ? (size_t)B * Hkv * (c.Lmax / c.page_size) * 4 : 0}; }
+
 // Rows x[b][t][h][0..hd) of heads and strides of their own.
 struct Rows {
     const void *p;
@@ -750,6 +775,38 @@ lvlm_status lvlm_kv_append(lvlm_ctx *ctx, void *stream, const lvlm_append_desc *
     if ((src->n_new && overlap(src->n_new, span(d->B, 1, d->Hkv, 1, d->n_stride_b, 0, d->n_stride_h, 4), len_out, heads)) ||
         (src->pos && overlap(src->pos, axes * d->B * d->T * 4, len_out, heads)))
         return fail(ctx, LVLM_ERR_INVALID_ARG, "kv_append: len_out overlaps n_new or pos");
+    const bool turns = d->rot_dim > 0, rows = d->T > 0;
+    const int eb = elem_bytes(d->dtype);
+    const size_t per_entry = rows ? span(d->B, 1, d->Hkv, d->T, d->m_stride_b, 0, d->m_stride_h, 1) : 0;
+    const auto row_range = [&](const void *p, int H, long long sb, long long st, long long sh) {
+        return Range{p, rows && p ? span(d->B, d->T, H, d->hd, sb, st, sh, eb) : 0};
+    };
+    Range out[kCacheRanges + 1], in[11];
+    cache_ranges(*cache, d->B, d->Hkv, (size_t)d->hd * eb, out);
+    out[kCacheRanges] = {len_out, heads};
+    in[0] = {src->pos, axes * d->B * d->T * 4};
+    in[1] = {src->inv_freq, turns ? (size_t)d->rot_dim * 2 : 0};
+    in[2] = {src->n_new, span(d->B, 1, d->Hkv, 1, d->n_stride_b, 0, d->n_stride_h, 4)};
+    in[3] = {src->score, per_entry * 4};
+    in[4] = {src->kind, per_entry};
+    in[5] = {src->orig_pos, per_entry * 4};
+    in[6] = page_range(*cache, d->B, d->Hkv);
+    in[7] = {len, len != len_out ? heads : 0};
+    in[8] = row_range(src->k, d->Hkv, d->k_stride_b, d->k_stride_t, d->k_stride_h);
+    in[9] = row_range(src->v, d->Hkv, d->v_stride_b, d->v_stride_t, d->v_stride_h);
+    in[10] = row_range(src->q, d->Hq, d->q_stride_b, d->q_stride_t, d->q_stride_h);
+    const char *why = check_apart(out, kCacheRanges + 1, in, 11);
+    if (!why && rows && src->q) {
+        // q_out against the rows: slices of one buffer may be in each other's ranges
+        const Rows qo{src->q_out, d->Hq, d->qo_stride_b, d->qo_stride_t, d->qo_stride_h};
+        if (rows_overlap({src->k, d->Hkv, d->k_stride_b, d->k_stride_t, d->k_stride_h}, qo, d->B, d->T, d->hd, eb) ||
+            rows_overlap({src->v, d->Hkv, d->v_stride_b, d->v_stride_t, d->v_stride_h}, qo, d->B, d->T, d->hd, eb))
+            why = "q_out overlaps the new rows";
+        const Range q_out = row_range(src->q_out, d->Hq, d->qo_stride_b, d->qo_stride_t, d->qo_stride_h);
+        if (!why) why = check_apart(&q_out, 1, in, 8);
+        if (!why) why = check_apart(&q_out, 1, out, kCacheRanges + 1);
+    }
+    if (why) return fail(ctx, LVLM_ERR_INVALID_ARG, "kv_append: %s", why);
     if (d->T == 0 && len == len_out) return LVLM_OK;
     const DeviceScope scope(ctx);
     if (lvlm_status st = scope.status(ctx)) return st;
@@ -777,6 +834,9 @@ lvlm_status lvlm_tree_attn(lvlm_ctx *ctx, void *stream, const lvlm_tree_desc *d,
     if (row_lse && (overlap(row_lse, lb, q, qb) || overlap(row_lse, lb, out, ob) || overlap(row_lse, lb, cache->k, cb) ||
                     overlap(row_lse, lb, cache->v, cb)))
         return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: row_lse overlaps q, out or the cache");
+    const Range written[] = {{out, ob}, {row_lse, lb}}, read[] = {{len, (size_t)d->B * d->Hkv * 4}, {n_rows, (size_t)d->B * 4},
+        {mask, (size_t)d->B * d->T * ((d->T + 31) / 32) * 4}, page_range(*cache, d->B, d->Hkv)};
+    if (const char *why = check_apart(written, 2, read, 4)) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_attn: %s", why);
     const TreeWs w = tree_ws(*d);
     if (lvlm_status st = need_ws(ctx, w.total)) return st;
     const DeviceScope scope(ctx);
@@ -796,6 +856,12 @@ lvlm_status lvlm_tree_commit(lvlm_ctx *ctx, void *stream, const lvlm_commit_desc
     const size_t heads = (size_t)d->B * d->Hkv * 4;
     if (overlap(path, (size_t)d->B * d->P * 4, len_out, heads) || overlap(n_path, (size_t)d->B * 4, len_out, heads))
         return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_commit: len_out overlaps path or n_path");
+    Range written[kCacheRanges + 1];
+    cache_ranges(*cache, d->B, d->Hkv, (size_t)d->hd * elem_bytes(d->dtype), written);
+    written[kCacheRanges] = {len_out, heads};
+    const Range read[] = {{path, (size_t)d->B * d->P * 4}, {n_path, (size_t)d->B * 4}, page_range(*cache, d->B, d->Hkv),
+                          {len, len != len_out ? heads : 0}};
+    if (const char *why = check_apart(written, kCacheRanges + 1, read, 4)) return fail(ctx, LVLM_ERR_INVALID_ARG, "tree_commit: %s", why);
     const DeviceScope scope(ctx);
     if (lvlm_status st = scope.status(ctx)) return st;
     return after_launch(ctx, launch_tree_commit(Prof{ctx, static_cast<hipStream_t>(stream)}, *d, *cache, len, path, n_path, len_out));

@@ -4,7 +4,7 @@ import pytest
 
 import paper_2509_00419_amd as lv
 import test_tree_abi as abi
-from test_tree_abi import K, LEN, LEN2, Q, V
+from test_tree_abi import FREQ, K, LEN, LEN2, MASK, NEW, NEWV, POS, Q, QO, TAB, V
 
 NOWHERE = 99        # a device that no machine has
 
@@ -57,9 +57,51 @@ def test_no_new_rows_read_nothing():
         assert st == 1 and "pos and inv_freq" in why
 
 
+# ---- outputs over what the call reads, or over each other ------------------------------------------------------------
+
+SCORE, KIND, ORIG, NEW_SCORE, NEW_KIND, NEW_ORIG, COUNTS, PATH, N_PATH, LSE = (x << 32 for x in range(20, 30))
+APPEND_READS = {"k": NEW, "v": NEWV, "q": Q, "pos": POS, "inv_freq": FREQ, "n_new": COUNTS, "score": NEW_SCORE, "kind": NEW_KIND, "orig_pos": NEW_ORIG}
+CACHE = {"k": K, "v": V, "score": SCORE, "kind": KIND, "orig_pos": ORIG, "pages": TAB, "page_size": 64, "n_pages": 32}
+
+
+def append(src=(), cache=(), length=(LEN, LEN2)):
+    return abi._append(desc={"n_stride_b": 1, "m_stride_b": 20, "m_stride_h": 5}, src={**APPEND_READS, "q_out": QO, **dict(src)},
+                       cache={**CACHE, **dict(cache)}, length=length)
+
+
 def refused(result):
     st, why = result
     return st == 1 and "overlap" in why
+
+
+def test_append_with_everything_given_passes():
+    assert passes(append()) and passes(append(length=(LEN, LEN))) and passes(append(src={"q_out": Q}))
+
+
+@pytest.mark.parametrize("read", [*APPEND_READS, "len", "pages"])
+@pytest.mark.parametrize("written", ["k", "v", "score", "kind", "orig_pos", "q_out", "len_out"])
+def test_append_refuses_an_output_over_what_it_reads(written, read):
+    if (written, read) in (("q_out", "q"), ("len_out", "len")):
+        pytest.skip("may be the same")
+    at = LEN if read == "len" else TAB if read == "pages" else APPEND_READS[read]
+    if written == "q_out":
+        assert refused(append(src={"q_out": at}))
+    elif written == "len_out":
+        assert refused(append(length=(LEN, at)))
+    else:
+        assert refused(append(cache={written: at}))
+
+
+@pytest.mark.parametrize("a,b", [(a, b) for i, a in enumerate(("k", "v", "score", "kind", "orig_pos")) for b in ("k", "v", "score", "kind", "orig_pos")[:i]])
+def test_a_cache_of_arrays_that_overlap_is_refused(a, b):
+    assert refused(append(cache={a: CACHE[b]}))
+    assert refused(commit(cache={a: CACHE[b]}))
+
+
+@pytest.mark.parametrize("a", ["k", "v", "score", "kind", "orig_pos"])
+def test_queries_and_lengths_over_the_cache_are_refused(a):
+    assert refused(append(src={"q_out": CACHE[a]})) and refused(append(length=(LEN, CACHE[a]))) and refused(commit(len_out=CACHE[a]))
+    assert refused(append(length=(LEN, QO)))
 
 
 def test_slices_of_one_buffer_do_not_overlap():
@@ -69,9 +111,12 @@ def test_slices_of_one_buffer_do_not_overlap():
     qo = {"qo_stride_b": 5 * row, "qo_stride_t": row}
     src = {"q": Q, "k": Q + 2 * 1024, "v": Q + 2 * 1536}
     assert passes(abi._append(desc={**strides, **qo}, src={**src, "q_out": Q}))
+    assert refused(abi._append(desc={**strides, **qo}, src={**src, "q_out": Q + 2 * 128}))            # reaches into k's rows
+    assert refused(abi._append(desc={**strides, **qo}, src={**src, "q_out": Q + 2 * 1024}))
     # q turned into a slice of its own behind v's
     wide = {f"{x}_stride_{a}": n for x in ("q", "qo", "k", "v") for a, n in (("b", 5 * (row + 1024)), ("t", row + 1024))}
     assert passes(abi._append(desc=wide, src={**src, "q_out": Q + 2 * row}))
+    assert refused(abi._append(desc=wide, src={**src, "q_out": Q + 2 * (row - 8)}))
     assert refused(abi._append(desc=wide, src={**src, "q_out": Q + 2 * (row + 8)}))                   # ... into the next row's q
     # heads before tokens, [B, heads, T, d]: the sequences' steps are what is left
     heads = {f"{x}_stride_{a}": n for x in ("q", "qo") for a, n in (("b", 16 * 5 * 128), ("t", 128), ("h", 5 * 128))}
@@ -80,3 +125,27 @@ def test_slices_of_one_buffer_do_not_overlap():
     # the same for attention
     both = {f"{x}_stride_{a}": n for x in ("q", "o") for a, n in (("b", 5 * row), ("t", row))}
     assert passes(abi._tree(desc=both, out=Q + 2 * 1024)) and refused(abi._tree(desc=both, out=Q + 2 * 1016))
+
+
+@pytest.mark.parametrize("read", [Q, K, V, LEN, COUNTS, MASK, TAB])
+def test_attention_refuses_an_output_over_what_it_reads(read):
+    pages = {"pages": TAB, "page_size": 64, "n_pages": 32}
+    assert passes(abi._tree(cache=pages, n_rows=COUNTS, lse=LSE))
+    assert refused(abi._tree(cache=pages, n_rows=COUNTS, lse=LSE, out=read)) and refused(abi._tree(cache=pages, n_rows=COUNTS, lse=read))
+
+
+def commit(cache=(), path=PATH, n_path=N_PATH, length=LEN, len_out=LEN2):
+    d = abi.bd.CommitDesc(abi.bd.BF16, 2, 4, 128, 5, 0)
+    ctx, c = lv.Context(NOWHERE), abi._cache(**{**CACHE, **dict(cache)})
+    st = abi.bd.lib.lvlm_tree_commit(ctx._h, None, abi.C.byref(d), abi.C.byref(c), length, path, n_path, len_out)
+    return st, abi.bd.lib.lvlm_last_error(ctx._h).decode()
+
+
+@pytest.mark.parametrize("read", [LEN, PATH, N_PATH, TAB])
+@pytest.mark.parametrize("written", ["k", "v", "score", "kind", "orig_pos", "len_out"])
+def test_commit_refuses_an_output_over_what_it_reads(written, read):
+    assert passes(commit()) and passes(commit(len_out=LEN))
+    if written == "len_out":
+        assert read == LEN or refused(commit(len_out=read))
+    else:
+        assert refused(commit(cache={written: read})) and refused(commit(cache={written: read}, len_out=LEN))
