@@ -149,3 +149,16 @@ def test_commit_refuses_an_output_over_what_it_reads(written, read):
         assert read == LEN or refused(commit(len_out=read))
     else:
         assert refused(commit(cache={written: read})) and refused(commit(cache={written: read}, len_out=LEN))
+
+
+def test_sizes_and_strides_at_their_limits():
+    """Ranges of 2^60 bytes: whatever is said of them is said without overflow."""
+    most = 1 << 36
+    strides = {f"{x}_stride_{a}": most for x in ("k", "v", "q", "qo") for a in "bth"}
+    small = {"n_stride_b": most, "n_stride_h": 0, "m_stride_b": most, "m_stride_h": most}
+    for B, T, H in ((65535, 1 << 22, 1024), (1, 1 << 22, 1), (65535, 1, 1)):
+        st, why = abi._append(desc={"B": B, "T": T, "Hq": H, "Hkv": H, **strides, **small}, src={"n_new": COUNTS, "kind": NEW_KIND},
+                              cache={**CACHE, "Lmax": 1 << 24, "page_size": 65536, "n_pages": (1 << 31) - 1})
+        assert st == 1 and "overlap" in why
+    tree = {f"{x}_stride_{a}": most for x in "qo" for a in "bth"}
+    assert refused(abi._tree(desc={"B": 65535, "T": 128, "Hq": 64, "Hkv": 2, **tree}))
