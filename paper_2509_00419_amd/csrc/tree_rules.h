@@ -14,8 +14,9 @@ constexpr int kSharePairs = 512, kShareRuns = 64;
 // entries.  Many rows to a workgroup read an entry for all of them at once; few rows make many workgroups of few tiles each; runs
 // make more still, and cost a second launch that folds their sums.  What a cut takes is put together from the numbers below, and
 // the cut that takes least is done.  The numbers are a fit to the times of 766 shapes (4 to 512 pairs, 1 to 1536 rows, 64 to
-// 16384 entries, both types and head dimensions) in all forms and up to 64 runs; the cut they choose takes 0.6 % longer than the
-// shape's best on average, 26 % at most.  Against splitting until there are 512 workgroups and 256 rows where there are more than
+// 16384 entries, both types and head dimensions) in all forms and up to 64 runs.  Of 778 timed once more with the present kernels the cut
+// they choose takes 2.8 % longer than the shape's best on average, more than 10 % in 46 and 50 % at most (16 x 1024 rows x 4500 entries of 64
+// channels).  Against splitting until there are 512 workgroups and 256 rows where there are more than
 // 128, us: 4 pairs x 28 rows x 512 entries of 128 channels 12.6 -> 7.8, 8 x 384 x 2048 35 -> 17, 32 x 384 x 512 32 -> 13, 64 x 1 x
 // 2048 23 -> 16, 128 x 192 x 2048 72 -> 44, 512 x 768 x 128 117 -> 70; with 256 rows where they are right 32 x 384 x 16384
 // 160 -> 134.
