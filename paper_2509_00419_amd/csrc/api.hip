@@ -7,6 +7,7 @@
 #include <string.h>
 
 #include <new>
+#include <numeric>
 
 #include "common.h"
 
@@ -217,26 +218,23 @@ struct Rows {
     int H;
     long long sb, st, sh;
 };
-// Do x and y share elements?  Where their ranges do, they may still be slices of one buffer that go through it in the same steps: all heads'
-// rows of a token in a part of the step of their own, or all tokens' of a sequence.  (Other ways past each other are taken for an overlap.)
+// Do x and y share elements?  Where their ranges do, they may still be parts of one buffer, beside each other along any axis: taken modulo
+// what the strides of some axes are multiples of, x and y are what their other axes span, and apart if those are.  (Other ways past
+// each other are taken for an overlap.)
 bool rows_overlap(const Rows &x, const Rows &y, int B, int T, int hd, int eb) {
     if (!overlap(x.p, span(B, T, x.H, hd, x.sb, x.st, x.sh, eb), y.p, span(B, T, y.H, hd, y.sb, y.st, y.sh, eb))) return false;
-    if (B > 1 && x.sb != y.sb) return true;
-    const auto apart = [&](long long step, size_t nx, size_t ny) {      // y from x, modulo the step, behind x's part and before the next x
-        if (step <= 0) return false;
+    const long long by = (long long)(reinterpret_cast<uintptr_t>(y.p) - reinterpret_cast<uintptr_t>(x.p));
+    for (int axes = 1; axes < 8; ++axes) {
+        const bool b = axes & 1, t = axes & 2, h = axes & 4;
+        long long step = 0;
+        for (const long long stride : {b && B > 1 ? x.sb : 0, b && B > 1 ? y.sb : 0, t && T > 1 ? x.st : 0, t && T > 1 ? y.st : 0,
+                                       h && x.H > 1 ? x.sh : 0, h && y.H > 1 ? y.sh : 0})
+            step = std::gcd(step, stride);
+        if (step == 0) continue;
         step *= eb;
-        const long long by = (long long)(reinterpret_cast<uintptr_t>(y.p) - reinterpret_cast<uintptr_t>(x.p)), r = (by % step + step) % step;
-        return r >= (long long)nx && step - r >= (long long)ny;
-    };
-    if (B > 1 && apart(x.sb, span(1, T, x.H, hd, 0, x.st, x.sh, eb), span(1, T, y.H, hd, 0, y.st, y.sh, eb))) return false;
-    if (T > 1 && x.st == y.st) {
-        long long step = x.st, rest = B > 1 ? x.sb : 0;
-        while (rest != 0) {                         // what both steps are multiples of
-            const long long r = step % rest;
-            step = rest;
-            rest = r;
-        }
-        if (apart(step, span(1, 1, x.H, hd, 0, 0, x.sh, eb), span(1, 1, y.H, hd, 0, 0, y.sh, eb))) return false;
+        const auto part = [&](const Rows &r) { return (long long)span(b ? 1 : B, t ? 1 : T, h ? 1 : r.H, hd, r.sb, r.st, r.sh, eb); };
+        const long long at = (by % step + step) % step;
+        if (at >= part(x) && step - at >= part(y)) return false;
     }
     return true;
 }

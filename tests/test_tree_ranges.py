@@ -162,3 +162,28 @@ def test_sizes_and_strides_at_their_limits():
         assert st == 1 and "overlap" in why
     tree = {f"{x}_stride_{a}": most for x in "qo" for a in "bth"}
     assert refused(abi._tree(desc={"B": 65535, "T": 128, "Hq": 64, "Hkv": 2, **tree}))
+
+
+@pytest.mark.parametrize("where", ["heads", "tokens", "sequences", "heads before tokens", "tokens before sequences"])
+def test_parts_of_any_axis_do_not_overlap(where):
+    """q, k and v of as many heads in one buffer, one part after the other along an axis; q turned in place, or into a fourth part."""
+    B, T, H, d = 2, 5, 4, 128
+    order = {"heads": "bth", "tokens": "bth", "sequences": "bth", "heads before tokens": "bht", "tokens before sequences": "tbh"}[where]
+    axis = {"heads": 3, "tokens": 2, "sequences": 0, "heads before tokens": 1, "tokens before sequences": 2}[where]
+    sizes = [{"b": B, "t": T, "h": H}[a] for a in order] + [d]
+    sizes.insert(axis, 4)                                               # q, k, v and q_out: a place of the parts' own among the axes
+    stride = [1] * 5
+    for i in range(3, -1, -1):
+        stride[i] = stride[i + 1] * sizes[i + 1]
+    part, stride = stride[axis], stride[:axis] + stride[axis + 1:]
+    step = {a: stride[order.index(a)] for a in "bth"}
+    desc = {f"{x}_stride_{a}": step[a] for x in ("q", "k", "v", "qo") for a in "bth"}
+    src = {"q": Q, "k": Q + 2 * part, "v": Q + 4 * part}
+    for at in range(4):
+        got = abi._append(desc={"Hq": H, **desc}, src={**src, "q_out": Q + 2 * at * part})
+        assert passes(got) if at in (0, 3) else refused(got), (at, got)
+        if at and part > 8:
+            got = abi._append(desc={"Hq": H, **desc}, src={**src, "q_out": Q + 2 * (at * part - 8)})
+            assert refused(got), (at, got)
+    tree = {f"{x}_stride_{a}": step[a] for x in "qo" for a in "bth"}
+    assert passes(abi._tree(desc={"Hq": H, **tree}, out=Q + 2 * part)) and refused(abi._tree(desc={"Hq": H, **tree}, out=Q + 2 * (part - 8)))
