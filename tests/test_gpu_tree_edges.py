@@ -1,9 +1,14 @@
 """GPU tests of the drafted-token calls at the edges of what they take."""
+import math
+
 import pytest
 import torch
 
 import paper_2509_00419_amd as lv
-from test_gpu_tree import BF, DEV, Caches
+import test_gpu_tree as tests
+from test_gpu_parity import _guarded
+from test_gpu_tree import BF, DEV, LONG, Caches
+from test_gpu_tree_cuts import CUTS
 
 pytestmark = pytest.mark.gpu
 
@@ -45,7 +50,6 @@ def test_far_positions_turn_as_exactly_as_near_ones(ctx, adjacent):
     """Unit keys and queries become the cosine and sine of their angles: 2^-25 of a turn off at most (2 pi 2^-25), by which either changes as
     much at most, and 4 ulp of a number up to 1 (2^-22) for the function itself; the products are with 1 and 0.  Frequencies of hundreds,
     positions near the last there are: 2^38 turns, of which one 64-bit word keeps 2^-15."""
-    import math
     from fractions import Fraction
     two_pi = 2 * Fraction("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803482534211706798214808651")
     T, d = 37, 64
@@ -91,3 +95,69 @@ def test_as_many_lists_as_a_call_may_have(ctx, dtype):
         x = q[b, h, 0].double() * k[b, h, 0].double() * d ** -0.5
         off = abs(float(lse[b, h, 0]) - float(x.sum()))
         assert off <= 2.0 ** -24 * ((d + 4) * float(x.abs().sum()) + 5 + 4 * abs(float(x.sum())))       # (as in test_gpu_tree.py)
+
+
+@pytest.mark.parametrize("case", [c for c in LONG[:16] + CUTS if c[7] == 0 and c[1] * c[4] <= 100], ids=lambda c: "-".join(map(str, c[1:7])))
+def test_tree_attention_stays_within_the_workspace_it_asked_for(case):
+    """A guard band behind exactly that many bytes; heads longer than the bound, empty, and in between."""
+    dtype, B, T, Hq, Hkv, d, slots = case[:7]
+    lens = torch.randint(0, 2 * slots, (B, Hkv), generator=torch.Generator().manual_seed(slots))
+    lens[0, 0], lens[-1, -1] = slots + 9, 0
+    c = Caches(dtype, lens.tolist(), slots + 9, d, 0, slots).dev()
+    q = torch.randn(B, T, Hq, d, generator=torch.Generator().manual_seed(T)).to(dtype).to(DEV)
+    _guarded(lambda context, reserve: context.tree_attn(q, c.k, c.v, c.len, len_bound=slots, reserve=reserve))
+
+
+@pytest.mark.parametrize("dtype", [BF, torch.float32])
+def test_append_and_commit_of_as_many_sequences_as_a_call_may_have(ctx, dtype):
+    """65535 sequences, counts that have to be clamped: entries where they belong, lengths, and what stays as it was."""
+    B, H, d, room, T = 65535, 2, 64, 4, 3
+    g = torch.Generator(device=DEV).manual_seed(9)
+    k, v = (torch.randn(B, T, H, d, generator=g, device=DEV).to(dtype) for _ in range(2))
+    kc, vc = (torch.zeros(B, H, room, d, dtype=dtype, device=DEV) for _ in range(2))
+    length = (torch.arange(B * H, device=DEV, dtype=torch.int32) % 2).view(B, H)
+    n = torch.randint(-2, T + 4, (B,), generator=g, device=DEV, dtype=torch.int32)
+    out, _ = ctx.kv_append(k, v, kc, vc, length, n_new=n)
+    took = n.clamp(0, T)
+    assert torch.equal(out, length + took[:, None])
+    slot = torch.arange(room, device=DEV).view(1, 1, room) - length.unsqueeze(-1)           # new row of each slot
+    held = (slot >= 0) & (slot < took.view(B, 1, 1))
+    for new, cache in ((k, kc), (v, vc)):
+        want = torch.gather(new.transpose(1, 2), 2, slot.clamp(0, T - 1).unsqueeze(-1).expand(-1, -1, -1, d).long())
+        assert torch.equal(cache, torch.where(held.unsqueeze(-1), want, torch.zeros_like(want)))
+    keep = kc.clone()
+    path = torch.tensor([[1, 2, 7]], dtype=torch.int32, device=DEV).expand(B, 3).contiguous()
+    done = ctx.tree_commit(kc, vc, length, path, took)
+    # rows 1 and 2 move to places 0 and 1 where they lie in the slots; row 7 never does
+    moved = torch.minimum(took, torch.full_like(took, 2)).view(B, 1)
+    assert torch.equal(done, length + moved)
+    for i in range(2):
+        here = moved > i
+        to, come = (length + i).long().clamp(max=room - 1), (length + i + 1).long().clamp(max=room - 1)
+        row = torch.gather(keep, 2, torch.where(here, come, to).view(B, H, 1, 1).expand(B, H, 1, d))
+        assert torch.equal(torch.gather(kc, 2, to.view(B, H, 1, 1).expand(B, H, 1, d)), row)
+
+
+@pytest.mark.parametrize("dtype,d", [(BF, 128), (torch.float32, 64)])
+def test_as_many_rows_as_a_list_may_have(ctx, dtype, d):
+    tests.test_every_cut_matches_the_formula(ctx, dtype, 1, 1024, 63, 1, d, 1100, 0, "tree")
+
+
+@pytest.mark.parametrize("dtype,T", [(BF, 1), (BF, 70), (torch.float32, 1), (torch.float32, 5)])
+def test_the_longest_list_there_can_be(ctx, dtype, T):
+    """2^24 slots of one head.  Queries of zero weigh all entries alike, so every sum is one of whole numbers below 2^25, and a row is the
+    mean of what it sees: as far as fp32 holds a quotient, and the fold's sums, 64 roundings of 2^-24."""
+    L, d = 1 << 24, 64
+    k, v = (torch.zeros(1, 1, L, d, dtype=dtype, device=DEV) for _ in range(2))
+    k.normal_(generator=torch.Generator(device=DEV).manual_seed(1))
+    v[0, 0, : L // 2] = 1.0
+    v[0, 0, L - T:] = 64.0
+    length = torch.tensor([[L]], dtype=torch.int32, device=DEV)
+    q = torch.zeros(1, T, 1, d, dtype=dtype, device=DEV)
+    out, lse = ctx.tree_attn(q, k, v, length, want_lse=True)
+    for t in range(T):
+        seen = L - T + t + 1
+        mean = (L // 2 + 64.0 * (t + 1)) / seen
+        step = 2.0 ** -8 if dtype == BF else 0.0
+        assert float((out[0, t, 0].double() - mean).abs().max()) <= mean * (72 * 2.0 ** -24 + step), t
+        assert abs(float(lse[0, 0, t]) - math.log(seen)) <= 72 * 2.0 ** -24 + 4 * 2.0 ** -24 * math.log(seen)
