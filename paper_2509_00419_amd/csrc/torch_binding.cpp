@@ -843,7 +843,8 @@ PyMethodDef methods[] = {
                 "length_out=None)\n--\n\n"
                 "lvlm_tree_commit (in place).  length [B,Hkv] before the drafts, path [B,P] ascending drafted rows, n_path [B];\n"
                 "returns length_out [B,Hkv] (length itself may be passed)."),
-    {"reserve", reserve, METH_O, "reserve($self, nbytes, /)\n--\n\nGrows the attached workspace (never shrinks); call outside graph capture."},
+    {"reserve", reserve, METH_O, "reserve($self, nbytes, /)\n--\n\nGrows the attached workspace (never shrinks); call outside graph capture.\n"
+                               "A captured graph keeps the workspace of its capture: reserve for the largest call before the first."},
     {"_attach", attach, METH_VARARGS, "The lvlm_ctx handle (an address, 0: none) and device the calls go to."},
     {nullptr, nullptr, 0, nullptr}};
 PyGetSetDef getset[] = {{"_ws", get_ws, set_ws, "the workspace tensor", nullptr}, {nullptr, nullptr, nullptr, nullptr, nullptr}};
